@@ -385,6 +385,95 @@ size_t cdl_workspace_bytes(int32_t op, int32_t M, int32_t N, int32_t K);
  * any other content, such as whatever a fresh or recycled allocation holds, reads as OK. */
 int cdl_workspace_status(void *ws, void *stream);
 
+/*
+ * ---------------------------------------------------------------------------------------------------------------
+ * Operators of language models (no counterpart in the paper): dropout, block-scaled 8-bit floating-point products with
+ * their quantizer, and the cross entropy over a large vocabulary.  The conventions at the top of this file hold.
+ * Element types of their tensors:
+ */
+#define CDL_F32 0  /* IEEE binary32 */
+#define CDL_BF16 1 /* bfloat16 */
+#define CDL_F16 2  /* IEEE binary16 */
+
+/*
+ * Counter-based dropout; the mask is never stored:
+ *   y[r,c] = (u_e >= p ? x[r,c] : 0) * RN(1 / (1 - p))  (+ residual[r,c]),     e = first_index + r * cols + c,
+ * u_e the uniform number of cdl_quantize_sample: the top 24 bits, times 2^-24, of word (e mod 4) of the Philox4x32-10 block
+ * with counter (e div 4, 0) and key `seed`.  The draw depends on (seed, e) alone: the backward pass is the same call on
+ * dL/dy without the residual (whose gradient is dL/dy itself), and any partition of a tensor into calls gives the same
+ * mask.  Computed in binary32 and rounded once.  A dropped element is 0 whatever x holds (NaN, infinities); p = 1 drops all.
+ *   x, y, residual [dev] rows x cols of `type`, row pitches ldx, ldy, ldr in elements (not read when rows = 1), aligned to
+ *   their element; 16-byte alignment, cols a multiple of 8 and first_index a multiple of 4 take the vector path.
+ *   residual nullable.  y may be x or residual.  rows = 0 or cols = 0 is valid.
+ * CDL_ERR_RANGE unless 0 <= p <= 1.
+ */
+int cdl_dropout(const void *x, int64_t ldx, const void *residual, int64_t ldr, void *y, int64_t ldy, int32_t type,
+                int64_t rows, int64_t cols, float p, uint64_t seed, uint64_t first_index, void *stream);
+
+/*
+ * Block-scaled 8-bit floating point: a matrix as e4m3 codes (4 exponent bits, 3 fraction bits, largest value 448, no
+ * infinities) with one binary32 scale per group of 128 consecutive entries of a row (CDL_FP8_ROWS) or per 128 x 128
+ * block (CDL_FP8_BLOCKS); groups at the edge are shorter.  An entry stands for code * scale.
+ *   s = max(RN(amax * RN(1/448)), 2^-126),  r = RN(1/s),  code = e4m3(RN(x * r))   to nearest, ties to even, saturated,
+ * amax the largest magnitude of the group (a NaN does not count).  NaN gets the NaN code; in a group with an infinity the
+ * scale is infinite, the infinities get the NaN code and the others 0.
+ *   x [dev] rows x cols of `type`, row pitch ldx (not read when rows = 1), aligned to its element.
+ *   codes [dev] rows x cols bytes, row pitch ldc;  scales [dev] floats [ceil(cols/128)][rows] (CDL_FP8_ROWS) or
+ *   [ceil(cols/128)][ceil(rows/128)] (CDL_FP8_BLOCKS): the layouts cdl_fp8_matmul reads.
+ *   codes_t, scales_t [dev], nullable together: the transposed matrix cols x rows, row pitch ldt, from the same read of x;
+ *   CDL_FP8_ROWS takes its groups along the rows of x (scales_t [ceil(rows/128)][cols]), CDL_FP8_BLOCKS gives the same
+ *   codes and scales transposed (scales_t [ceil(rows/128)][ceil(cols/128)]).
+ *   codes, codes_t 16-byte aligned, ldc, ldt multiples of 16; bytes between a row's end and the next are not written.
+ * rows = 0 or cols = 0 is valid.
+ */
+#define CDL_FP8_ROWS 0
+#define CDL_FP8_BLOCKS 1
+int cdl_fp8_quantize(const void *x, int64_t ldx, int32_t type, int32_t rows, int32_t cols, int32_t mode,
+                     void *codes, int64_t ldc, float *scales, void *codes_t, int64_t ldt, float *scales_t, void *stream);
+
+/*
+ * Product of two block-scaled 8-bit matrices, reduced along their rows:
+ *   out[m,n] = sum_kb sa(kb,m) * sb(kb,n) * ( sum_{k in block kb} A[m,k] * B[n,k] )  (+ bias[n])
+ * blocks of 128 along k; all sums in binary32, rounded once to out_type.  With codes from cdl_fp8_quantize:
+ *   forward          Y[tokens, out]  = X W^T     A = X (rows),        B = W (blocks or rows)
+ *   data gradient    dX[tokens, in]  = dY W      A = dY (rows),       B = W transposed (blocks)
+ *   weight gradient  dW[out, in]     = dY^T X    A = dY transposed,   B = X transposed (both rows, groups along tokens)
+ *   A [dev] M x K codes (pitch lda), a_scale [dev] [ceil(K/128)][M];  B [dev] N x K codes (pitch ldb), b_scale [dev]
+ *   [ceil(K/128)][N] (b_mode CDL_FP8_ROWS) or [ceil(K/128)][ceil(N/128)] (CDL_FP8_BLOCKS);  out [dev] M x N of out_type
+ *   (pitch ldo, in elements);  bias [dev] N floats, nullable.
+ *   A, B 16-byte aligned, lda, ldb multiples of 16; out aligned to its element (16-byte alignment of base and pitch
+ *   stores through TMA).
+ *   ws [dev]: cdl_fp8_matmul_workspace_bytes(M, N, K) bytes, 256-byte aligned (status block, see cdl_workspace_status).
+ * M = 0 or N = 0 is valid; K = 0 gives the bias or 0.  The result does not depend on what else runs: sums have a fixed order.
+ */
+int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, const void *B, int64_t ldb, const float *b_scale,
+                   int32_t b_mode, int32_t M, int32_t N, int32_t K, void *out, int64_t ldo, int32_t out_type,
+                   const float *bias, void *ws, size_t ws_bytes, void *stream);
+size_t cdl_fp8_matmul_workspace_bytes(int32_t M, int32_t N, int32_t K);
+
+/*
+ * Softmax cross entropy of the logits H W^T over a vocabulary of V words, the logits never stored:
+ *   l[t,v] = sum_d H[t,d] W[v,d],   lse[t] = log sum_v exp l[t,v],   loss[t] = lse[t] - l[t, labels[t]]
+ * A label outside 0..V-1 marks a position without a loss: loss[t] = 0 and no gradient (lse[t] is still written).
+ *   H [dev] T x D, W [dev] V x D of `type` (CDL_BF16 or CDL_F16), pitches ldh, ldw;  labels [dev] T int64;
+ *   loss, lse [dev] T floats.  Products and sums in binary32.
+ * The backward call takes lse from the forward call and dloss[t] = dL/dloss[t] [dev] (1 / count for a mean; not read where the
+ * label is outside) and gives
+ *   dl[t,v] = dloss[t] * (exp(l[t,v] - lse[t]) - [v = labels[t]]),   dH = dl W,   dW = dl^T H
+ * It goes through the vocabulary in pieces, recomputes each piece's logits and rounds dl, divided by the largest |dloss|, to
+ * 16 bits for the two products.
+ *   dH [dev] T x D (pitch lddh), dW [dev] V x D (pitch lddw) of `type`, each nullable; overwritten.
+ *   H, W, dH, dW 16-byte aligned, pitches multiples of 8.
+ *   ws [dev]: cdl_vocab_loss_workspace_bytes(T, V, D, with_gradient) bytes, 256-byte aligned (the larger size serves both).
+ * T = 0 is valid (dW is cleared); V and D at least 1.  The results have a fixed order of summation.
+ */
+int cdl_vocab_loss_fwd(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels,
+                       int32_t T, int32_t V, int32_t D, float *loss, float *lse, void *ws, size_t ws_bytes, void *stream);
+int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels,
+                       const float *lse, const float *dloss, int32_t T, int32_t V, int32_t D, void *dH, int64_t lddh,
+                       void *dW, int64_t lddw, void *ws, size_t ws_bytes, void *stream);
+size_t cdl_vocab_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t with_gradient);
+
 /* Static, NUL-terminated description of a status code. */
 const char *cdl_strerror(int status);
 

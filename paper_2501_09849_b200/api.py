@@ -15,6 +15,8 @@ __all__ = [
     "cdl_index_entropy", "cdl_qlinear_fwd", "cdl_qlinear_bwd", "cdl_qlinear_bwd_dw_noalloc", "cdl_noalloc_status",
     "cdl_workspace_bytes", "cdl_workspace_status", "cdl_rescale_acc", "CDL_NOALLOC_MAX_DW_ELEMS",
     "cdl_huffman_lengths", "cdl_qconv_bwd_fp", "cdl_qconv_bwd_fp_workspace_bytes", "cdl_qlinear_bwd_fp", "cdl_qlinear_bwd_fp_workspace_bytes", "cdl_qlinear_fwd_next", "cdl_qconv_fwd_next", "ConvShape", "cdl_qconv_fwd", "cdl_qconv_bwd", "cdl_qconv_workspace_bytes",
+    "cdl_dropout", "cdl_fp8_quantize", "cdl_fp8_matmul", "cdl_fp8_matmul_workspace_bytes", "cdl_vocab_loss_fwd", "cdl_vocab_loss_bwd",
+    "cdl_vocab_loss_workspace_bytes", "CDL_F32", "CDL_BF16", "CDL_F16", "CDL_FP8_ROWS", "CDL_FP8_BLOCKS",
     "CDL_HIST_ACCUMULATE", "CDL_OP_QLINEAR_FWD", "CDL_OP_QLINEAR_BWD", "CDL_MAX_LEVELS",
 ]
 
@@ -23,6 +25,8 @@ CDL_OP_QLINEAR_FWD = 1
 CDL_OP_QLINEAR_BWD = 2
 CDL_MAX_LEVELS = 256
 CDL_NOALLOC_MAX_DW_ELEMS = 1 << 20
+CDL_F32, CDL_BF16, CDL_F16 = 0, 1, 2
+CDL_FP8_ROWS, CDL_FP8_BLOCKS = 0, 1
 
 _PKG = Path(__file__).resolve().parent
 _LIB = None
@@ -121,7 +125,17 @@ def load_library():
     lib.cdl_rescale_acc.argtypes = [P, I32, I64, C.c_float, C.c_float, P, P]
     lib.cdl_rescale_acc.restype = C.c_int
     lib.cdl_noalloc_status.restype = C.c_int
-    for name in ("cdl_quantize_hard", "cdl_quantize_soft", "cdl_quantize_backward", "cdl_quantize_sample", "cdl_index_entropy",
+    lib.cdl_dropout.argtypes = [P, I64, P, I64, P, I64, I32, I64, I64, C.c_float, C.c_uint64, C.c_uint64, P]
+    lib.cdl_fp8_quantize.argtypes = [P, I64, I32, I32, I32, I32, P, I64, P, P, I64, P, P]
+    lib.cdl_fp8_matmul.argtypes = [P, I64, P, P, I64, P, I32, I32, I32, I32, P, I64, I32, P, P, C.c_size_t, P]
+    lib.cdl_fp8_matmul_workspace_bytes.argtypes = [I32, I32, I32]
+    lib.cdl_fp8_matmul_workspace_bytes.restype = C.c_size_t
+    lib.cdl_vocab_loss_fwd.argtypes = [P, I64, P, I64, I32, P, I32, I32, I32, P, P, P, C.c_size_t, P]
+    lib.cdl_vocab_loss_bwd.argtypes = [P, I64, P, I64, I32, P, P, P, I32, I32, I32, P, I64, P, I64, P, C.c_size_t, P]
+    lib.cdl_vocab_loss_workspace_bytes.argtypes = [I32, I32, I32, I32]
+    lib.cdl_vocab_loss_workspace_bytes.restype = C.c_size_t
+    for name in ("cdl_dropout", "cdl_fp8_quantize", "cdl_fp8_matmul", "cdl_vocab_loss_fwd", "cdl_vocab_loss_bwd",
+                 "cdl_quantize_hard", "cdl_quantize_soft", "cdl_quantize_backward", "cdl_quantize_sample", "cdl_index_entropy",
                  "cdl_qlinear_fwd", "cdl_qlinear_bwd", "cdl_qlinear_bwd_dw_noalloc", "cdl_workspace_status",
                  "cdl_qconv_fwd", "cdl_qconv_bwd"):
         getattr(lib, name).restype = C.c_int
@@ -132,20 +146,24 @@ def load_library():
 def _ptr(t):
     if t is None:
         return None
-    if isinstance(t, int):
-        return C.c_void_p(t)
-    return C.c_void_p(t.data_ptr())
+    return t if isinstance(t, int) else t.data_ptr()      # (declared argument types turn the number into a pointer)
+
+
+_CURRENT_STREAM = None      # () -> raw handle of torch's current stream on the current device
 
 
 def _stream(stream):
+    global _CURRENT_STREAM
     if stream is None:
-        import torch
-        if not torch.cuda.is_available():   # no device: the call fails in the library, not here
-            return None
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
-    if isinstance(stream, int):
-        return C.c_void_p(stream)
-    return C.c_void_p(stream.cuda_stream)
+        if _CURRENT_STREAM is None:
+            import torch
+            if not torch.cuda.is_available():   # no device: the call fails in the library, not here
+                return None
+            torch.cuda.init()
+            raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+            _CURRENT_STREAM = lambda: raw(device())      # what torch.cuda.current_stream() wraps in an object
+        return _CURRENT_STREAM()
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _check(rc, where, check):
@@ -353,3 +371,44 @@ def cdl_noalloc_status(stream=None, check=True):
 def cdl_rescale_acc(acc, acc_bits, n, q_x, q_y, out, stream=None, check=True):
     rc = load_library().cdl_rescale_acc(_ptr(acc), acc_bits, n, float(q_x), float(q_y), _ptr(out), _stream(stream))
     return _check(rc, "cdl_rescale_acc", check)
+
+
+def cdl_dropout(x, ldx, residual, ldr, y, ldy, type, rows, cols, p, seed, first_index=0, stream=None, check=True):
+    """Counter-based dropout (+ residual); the backward pass is the same call on the gradient with residual=None."""
+    rc = load_library().cdl_dropout(_ptr(x), ldx, _ptr(residual), ldr, _ptr(y), ldy, type, rows, cols, float(p), int(seed),
+                                    int(first_index), _stream(stream))
+    return _check(rc, "cdl_dropout", check)
+
+
+def cdl_fp8_quantize(x, ldx, type, rows, cols, mode, codes, ldc, scales, codes_t=None, ldt=0, scales_t=None, stream=None, check=True):
+    rc = load_library().cdl_fp8_quantize(_ptr(x), ldx, type, rows, cols, mode, _ptr(codes), ldc, _ptr(scales), _ptr(codes_t), ldt,
+                                         _ptr(scales_t), _stream(stream))
+    return _check(rc, "cdl_fp8_quantize", check)
+
+
+def cdl_fp8_matmul_workspace_bytes(M, N, K) -> int:
+    return int(load_library().cdl_fp8_matmul_workspace_bytes(M, N, K))
+
+
+def cdl_fp8_matmul(A, lda, a_scale, B, ldb, b_scale, b_mode, M, N, K, out, ldo, out_type, bias=None, ws=None, ws_bytes=0, stream=None,
+                   check=True):
+    rc = load_library().cdl_fp8_matmul(_ptr(A), lda, _ptr(a_scale), _ptr(B), ldb, _ptr(b_scale), b_mode, M, N, K, _ptr(out), ldo,
+                                       out_type, _ptr(bias), _ptr(ws), ws_bytes, _stream(stream))
+    return _check(rc, "cdl_fp8_matmul", check)
+
+
+def cdl_vocab_loss_workspace_bytes(T, V, D, with_gradient) -> int:
+    return int(load_library().cdl_vocab_loss_workspace_bytes(T, V, D, int(with_gradient)))
+
+
+def cdl_vocab_loss_fwd(H, ldh, W, ldw, type, labels, T, V, D, loss, lse, ws=None, ws_bytes=0, stream=None, check=True):
+    rc = load_library().cdl_vocab_loss_fwd(_ptr(H), ldh, _ptr(W), ldw, type, _ptr(labels), T, V, D, _ptr(loss), _ptr(lse), _ptr(ws),
+                                           ws_bytes, _stream(stream))
+    return _check(rc, "cdl_vocab_loss_fwd", check)
+
+
+def cdl_vocab_loss_bwd(H, ldh, W, ldw, type, labels, lse, dloss, T, V, D, dH=None, lddh=0, dW=None, lddw=0, ws=None, ws_bytes=0,
+                       stream=None, check=True):
+    rc = load_library().cdl_vocab_loss_bwd(_ptr(H), ldh, _ptr(W), ldw, type, _ptr(labels), _ptr(lse), _ptr(dloss), T, V, D, _ptr(dH),
+                                           lddh, _ptr(dW), lddw, _ptr(ws), ws_bytes, _stream(stream))
+    return _check(rc, "cdl_vocab_loss_bwd", check)

@@ -17,7 +17,7 @@ LIB = PKG / "libcdl.so"
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-DNDEBUG",
-    "-shared", "-cudart", "static",
+    "-shared", "-cudart", "static", "--threads", "0",
 ]
 
 

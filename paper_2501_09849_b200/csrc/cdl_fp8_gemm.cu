@@ -1,0 +1,528 @@
+// Block-scaled product of 8-bit floating-point operands on the tensor cores of sm_100a:
+//   out[m,n] = sum_kb sa[kb][m] * sb[kb][n or n / 128] * ( sum_{k in block kb of 128} A[m,k] B[n,k] )  (+ bias[n])
+// A [M][K] and B [N][K] are e4m3 codes with the reduced dimension contiguous; the inner sum is one 128-byte pipeline
+// stage: four tcgen05.mma (kind::f8f6f4, K = 32 each) into TMEM in binary32.
+//
+// The scales change with every stage, so an accumulator cannot stay in TMEM over the whole reduction: each stage's partial
+// tile goes into the next of the TMEM buffers, the epilogue warps read it back while the following stages' products run,
+// and add it, scaled, to the tile they keep in registers (one fused multiply-add per entry and stage; one more product
+// where B's scales change from column to column).  For a 256 x 256 tile of a CTA pair a stage is 512 tensor-core cycles
+// per SM, against 256 cycles of TMEM reads and 256 (or 512) of binary32 arithmetic for the 128 x 256 entries of a CTA.
+//
+// Tiles: 256 x 256 per CTA pair (cta_group::2, as in the index products), or 128 x 128 per CTA where the pair tiles would
+// leave SMs idle.  With few tiles (one token, a short prompt) the reduced dimension is also cut over the CTAs of a
+// cluster, whose partial tiles are added in a fixed order through distributed shared memory: no scratch in global
+// memory, no atomics, one launch.  Rows beyond M are zero-filled by TMA and cost no memory traffic.
+// Warp roles: warp 0 issues TMA, warp 1 owns TMEM and issues the MMAs, warps 4..11 are the epilogue.  Every wait is bounded.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <string.h>
+
+#include "cdl_internal.h"
+#include "cdl_lowp.cuh"
+#include "cdl_tc.cuh"
+#include "cdl_wait.cuh"
+
+namespace cdl {
+namespace {
+
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 128 + 32 * kEpiWarps;         // a warpgroup of which two warps drive the pipeline, two of epilogue warps
+// Registers: a pair's epilogue thread holds 128 sums besides the 32 partial ones it has just read, more than an even share
+// of the register file (168 for 384 threads).  The first warpgroup gives up what it does not need:
+// 128 * 88 + 256 * 208 = 384 * 168.
+constexpr int kRegsLaunch = 168, kRegsDrive = 88, kRegsEpilogue = 208;
+static_assert(128 * kRegsDrive + 32 * kEpiWarps * kRegsEpilogue <= kThreads * kRegsLaunch, "register shares");
+constexpr int kBlockBytes = 128 * 128;                 // one operand block of a stage: 128 rows x 128 bytes
+constexpr int kStageBytes = 2 * kBlockBytes;
+constexpr int kOutWarpBytes = 32 * 128;                // output staging of one epilogue warp
+constexpr int kStagesMax = 6;
+__host__ __device__ constexpr int stages(bool bvec) { return bvec ? 5 : 6; }
+__host__ __device__ constexpr int smem_bytes(bool bvec)
+{
+    return 1024 + stages(bvec) * kStageBytes + kEpiWarps * kOutWarpBytes + (bvec ? kEpiWarps * 2 * 128 * 4 : 0);
+}
+constexpr int kMaxSplits = 8;                          // portable cluster size
+constexpr unsigned long long kWaitNs = 2000000000ull;
+
+struct Fp8Params {
+    int M, N, KB;                   // KB: blocks of 128 along the reduced dimension
+    int tiles_i, tiles_j, slots;
+    int splits;                     // CTAs of a cluster that share a tile (single-CTA tiles only)
+    int nb;                         // scales of a k-block of B: N, or ceil(N / 128)
+    const float *sa, *sb, *bias;
+    void *out;
+    long long ldo;
+    int out_tma;                    // the output goes through shared memory and TMA
+    int *status;
+};
+
+// Tiles in bands of eight tile rows, columns outer, so that what runs at one time shares operand blocks in L2.
+__device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti, int &tj)
+{
+    const int band = 8 * tiles_j;
+    const int b = u / band, first = b * 8, rows = min(8, tiles_i - first), in = u - b * band;
+    tj = in / rows;
+    ti = first + in - tj * rows;
+}
+
+template <bool PAIR, bool BVEC, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                const __grid_constant__ CUtensorMap map_o, const Fp8Params P)
+{
+    extern __shared__ unsigned char smem_dyn[];
+    __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 8];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ int abort_s;
+
+    constexpr int kStages = stages(BVEC);
+    constexpr int kBufs = PAIR ? 2 : 4;                // TMEM buffers of a partial tile
+    constexpr int kTN = PAIR ? 256 : 128;
+    constexpr int kCols = kTN / 2;                     // columns of an epilogue warp
+    const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *abort_flag = &abort_s;
+    const uint32_t rank = PAIR || P.splits > 1 ? cluster_ctarank() : 0u;
+    const int slot = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x / P.splits;
+    const int split = PAIR ? 0 : (int)rank;
+    const int kb0 = PAIR ? 0 : (int)((long long)P.KB * split / P.splits);
+    const int kb1 = PAIR ? P.KB : (int)((long long)P.KB * (split + 1) / P.splits);
+    const int units = P.tiles_i * P.tiles_j;
+
+    const uint32_t bar0 = smem_u32(&bars[0]);
+    constexpr uint32_t kEmptyOff = 8u * kStagesMax;
+    const uint32_t tfull0 = bar0 + 16u * kStagesMax, tempty0 = tfull0 + 8u * kBufs;
+    if (threadIdx.x == 0) {
+        abort_s = 0;
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(bar0 + 8u * s, 1);
+            mbar_init(bar0 + kEmptyOff + 8u * s, 1);
+        }
+        for (int b = 0; b < kBufs; ++b) {
+            mbar_init(tfull0 + 8u * b, 1);
+            mbar_init(tempty0 + 8u * b, PAIR ? 2 * kEpiWarps : kEpiWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc_all<PAIR>(smem_u32(&tmem_base_s));
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_s;
+    bool failed = false;
+
+    if (warp < 4) {
+        if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsDrive));
+        if (warp == 0) {
+            // ------------------------------------------------------------ TMA producer (one lane)
+            if (lane == 0) {
+                uint32_t st = 0u, par = 1u;
+                for (int u = slot; u < units && !failed; u += P.slots) {
+                    int ti, tj;
+                    tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+                    const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
+                    const int brow = tj * kTN + (PAIR ? (int)rank * 128 : 0);
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        const uint32_t fb = bar0 + 8u * st;
+                        if (!mbar_try_wait_now(fb + kEmptyOff, par) && !mbar_wait(fb + kEmptyOff, par, abort_flag, kWaitNs)) {
+                            failed = true;
+                            break;
+                        }
+                        const uint32_t sa = smem_base + st * (uint32_t)kStageBytes, sb = sa + kBlockBytes;
+                        if (!PAIR || rank == 0) mbar_expect_tx(fb, (PAIR ? 2u : 1u) * (uint32_t)kStageBytes);
+                        if (PAIR) {
+                            tma_load_2d_pair(sa, &map_a, kb * 128, arow, fb);
+                            tma_load_2d_pair(sb, &map_b, kb * 128, brow, fb);
+                        } else {
+                            tma_load_2d(sa, &map_a, kb * 128, arow, fb);
+                            tma_load_2d(sb, &map_b, kb * 128, brow, fb);
+                        }
+                        if (++st == (uint32_t)kStages) {
+                            st = 0u;
+                            par ^= 1u;
+                        }
+                    }
+                }
+            }
+        } else if (warp == 1) {
+            // ------------------------------------------------------------ MMA issuer (one lane; CTA 0 of a pair)
+            if (lane == 0 && (!PAIR || rank == 0)) {
+                const uint64_t a_d = make_desc(smem_base, 16, 1024), b_d = make_desc(smem_base + kBlockBytes, 16, 1024);
+                const uint32_t a_hi = (uint32_t)(a_d >> 32), b_hi = (uint32_t)(b_d >> 32), a_lo0 = (uint32_t)a_d, b_lo0 = (uint32_t)b_d;
+                // D binary32, A and B e4m3, both K-major
+                const uint32_t idesc = (1u << 4) | ((uint32_t)(kTN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
+                uint32_t st = 0u, par = 0u, buf = 0u, tpar = 1u;
+                for (int u = slot; u < units && !failed; u += P.slots) {
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        const uint32_t fb = bar0 + 8u * st;
+                        if ((!mbar_try_wait_now(tempty0 + 8u * buf, tpar) && !mbar_wait(tempty0 + 8u * buf, tpar, abort_flag, kWaitNs)) ||
+                            (!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs))) {
+                            failed = true;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t off = st * (uint32_t)(kStageBytes >> 4);
+                        tc_mma4<PAIR, KIND_F8F6F4>(tmem_base + buf * (uint32_t)kTN, a_lo0 + off, a_hi, 2u, b_lo0 + off, b_hi, 2u, idesc, 0u);
+                        if (PAIR) {
+                            tc_commit_pair(fb + kEmptyOff);
+                            tc_commit_pair(tfull0 + 8u * buf);
+                        } else {
+                            tc_commit(fb + kEmptyOff);
+                            tc_commit(tfull0 + 8u * buf);
+                        }
+                        if (++st == (uint32_t)kStages) {
+                            st = 0u;
+                            par ^= 1u;
+                        }
+                        if (++buf == (uint32_t)kBufs) {
+                            buf = 0u;
+                            tpar ^= 1u;
+                        }
+                    }
+                }
+            }
+        }
+    } else {
+        if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
+        // ------------------------------------------------------------ epilogue warps
+        float2 acc[kCols / 2];
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t wbuf = smem_base + (uint32_t)(kStages * kStageBytes) + (uint32_t)((warp - 4) * kOutWarpBytes);
+        float *sbuf = reinterpret_cast<float *>(smem_dyn + (smem_base - smem_u32(smem_dyn)) + kStages * kStageBytes + kEpiWarps * kOutWarpBytes) +
+                      (warp - 4) * 256;
+        uint32_t buf = 0u, tpar = 0u;
+        constexpr int kLaneCols = kCols / 32;           // column scales a lane fetches per stage (BVEC)
+        for (int u = slot; u < units && !failed; u += P.slots) {
+            int ti, tj;
+            tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+            const int row0 = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
+            const int col0 = tj * kTN + half * kCols;
+            const int row = row0 + lane;
+            // scales two stages ahead of their use
+            auto load_sa = [&](int kb) { return row < P.M && kb < kb1 ? __ldg(P.sa + (long long)kb * P.M + row) : 0.0f; };
+            auto load_sb = [&](int kb, float (&s)[4]) {
+                if (BVEC) {
+#pragma unroll
+                    for (int j = 0; j < kLaneCols; ++j) {
+                        const int c = col0 + lane * kLaneCols + j;
+                        s[j] = c < P.N && kb < kb1 ? __ldg(P.sb + (long long)kb * P.N + c) : 0.0f;
+                    }
+                } else {
+                    s[0] = col0 < P.N && kb < kb1 ? __ldg(P.sb + (long long)kb * P.nb + (col0 >> 7)) : 0.0f;
+                }
+            };
+            float sa0 = load_sa(kb0), sa1 = load_sa(kb0 + 1);
+            float sb0[4], sb1[4];
+            load_sb(kb0, sb0);
+            load_sb(kb0 + 1, sb1);
+#pragma unroll
+            for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
+            if (BVEC) __syncwarp();                      // the last tile's column scales have been read
+            for (int kb = kb0; kb < kb1; ++kb) {
+                const float sa = sa0;
+                const float s_row = BVEC ? sa : sa * sb0[0];
+                float *sv = sbuf + (kb & 1) * 128;
+                if (BVEC) {
+                    if (kLaneCols == 4) *reinterpret_cast<float4 *>(sv + lane * 4) = make_float4(sb0[0], sb0[1], sb0[2], sb0[3]);
+                    else *reinterpret_cast<float2 *>(sv + lane * 2) = make_float2(sb0[0], sb0[1]);
+                    __syncwarp();
+                }
+                sa0 = sa1;
+                sa1 = load_sa(kb + 2);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sb0[j] = sb1[j];
+                load_sb(kb + 2, sb1);
+                const uint32_t tf = tfull0 + 8u * buf;
+                if (!__all_sync(0xffffffffu, mbar_try_wait_now(tf, tpar) || mbar_wait(tf, tpar, abort_flag, kWaitNs))) {
+                    failed = true;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * (uint32_t)kTN + (uint32_t)(half * kCols);
+#pragma unroll
+                for (int ch = 0; ch < kCols / 32; ++ch) {
+                    uint32_t v[32];
+                    tc_ld32(taddr + (uint32_t)(ch * 32), v);
+                    tc_wait_ld_pin(v);
+                    if (ch == kCols / 32 - 1) {          // the partial tile is in registers: its buffer is free
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (PAIR) mbar_arrive_remote(tempty0 + 8u * buf, 0u);
+                            else mbar_arrive(tempty0 + 8u * buf);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float2 s = make_float2(s_row, s_row);
+                        if (BVEC) s = mul2(s, *reinterpret_cast<const float2 *>(sv + ch * 32 + 2 * j));
+                        fma2(acc[ch * 16 + j], v[2 * j], v[2 * j + 1], s);
+                    }
+                }
+                if (++buf == (uint32_t)kBufs) {
+                    buf = 0u;
+                    tpar ^= 1u;
+                }
+            }
+            if (failed) break;
+            if (!PAIR && P.splits > 1) {
+                // The partial tile, [rows][128] binary32, takes the place of the pipeline's stages: this warp has seen the
+                // last of the CTA's products, so all loads have landed and been read.  16-byte units of a row are
+                // exclusive-ored with the row number: eight rows at a time hit all banks.
+                float *part = reinterpret_cast<float *>(smem_dyn + (smem_base - smem_u32(smem_dyn)));
+                const int r = quarter * 32 + lane;
+                if (row < P.M) {
+#pragma unroll
+                    for (int j = 0; j < kCols / 4; ++j) {
+                        const int unit = half * (kCols / 4) + j;
+                        *reinterpret_cast<float4 *>(part + r * 128 + ((unit ^ (r & 7)) << 2)) =
+                            make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
+                    }
+                }
+                break;
+            }
+            if (row0 >= P.M || col0 >= P.N) continue;
+            if (P.bias != nullptr) {
+#pragma unroll
+                for (int j = 0; j < kCols / 2; ++j) {
+                    if (col0 + 2 * j < P.N) acc[j].x += __ldg(P.bias + col0 + 2 * j);
+                    if (col0 + 2 * j + 1 < P.N) acc[j].y += __ldg(P.bias + col0 + 2 * j + 1);
+                }
+            }
+            if (P.out_tma) {
+                // 128-byte pieces of the warp's 32 rows through its staging block: TMA clips at the edges
+                constexpr int kPiece = 128 / (int)sizeof(T);
+#pragma unroll
+                for (int pc = 0; pc < kCols / kPiece; ++pc) {
+                    if (col0 + pc * kPiece >= P.N) break;
+                    if (lane == 0) bulk_wait_read<0>();
+                    __syncwarp();
+                    const uint32_t dst = wbuf + (uint32_t)lane * 128u;
+#pragma unroll
+                    for (int c4 = 0; c4 < 8; ++c4) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (sizeof(T) == 4) {
+                                const float2 a = acc[(pc * 32 + c4 * 4 + j) / 2];
+                                w[j] = __float_as_uint((j & 1) ? a.y : a.x);
+                            } else {
+                                const float2 a = acc[pc * 32 + c4 * 4 + j];
+                                w[j] = pack2<T>(a.x, a.y);
+                            }
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c4 ^ (lane & 7)) << 4)),
+                                     "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                                     : "memory");
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&map_o, col0 + pc * kPiece, row0, wbuf);
+                        bulk_commit();
+                    }
+                }
+            } else if (row < P.M) {
+                T *o = static_cast<T *>(P.out) + (long long)row * P.ldo + col0;
+#pragma unroll
+                for (int j = 0; j < kCols / 2; ++j) {
+                    if (col0 + 2 * j < P.N) o[2 * j] = from_f32<T>(acc[j].x);
+                    if (col0 + 2 * j + 1 < P.N) o[2 * j + 1] = from_f32<T>(acc[j].y);
+                }
+            }
+        }
+        if (lane == 0) bulk_wait_all();
+    }
+    if (failed) {
+        abort_s = 1;
+        if (lane == 0) record_timeout(P.status);
+    }
+
+    if (!PAIR && P.splits > 1) {
+        // each CTA adds its share of the tile's entries over the cluster's partial tiles, in the order of the splits
+        int ti, tj;
+        tile_at(slot, P.tiles_i, P.tiles_j, ti, tj);
+        const int rows = min(128, P.M - ti * 128), cols = min(128, P.N - tj * 128);
+        __syncthreads();
+        cluster_sync_all();
+        const int n4 = rows * 32;
+        for (int i = (int)rank * kThreads + (int)threadIdx.x; i < n4; i += P.splits * kThreads) {
+            const int r = i >> 5, unit = i & 31, c = unit * 4;
+            if (c >= cols) continue;
+            const uint32_t local = smem_base + (uint32_t)(r * 128 + ((unit ^ (r & 7)) << 2)) * 4u;
+            float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int s = 0; s < P.splits; ++s) {
+                float4 v;
+                asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\t"
+                             "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+                             : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                             : "r"(local), "r"(s));
+                sum.x += v.x;
+                sum.y += v.y;
+                sum.z += v.z;
+                sum.w += v.w;
+            }
+            const float o4[4] = {sum.x, sum.y, sum.z, sum.w};
+            T *o = static_cast<T *>(P.out) + (long long)(ti * 128 + r) * P.ldo + tj * 128 + c;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < cols) o[j] = from_f32<T>(o4[j] + (P.bias != nullptr ? __ldg(P.bias + tj * 128 + c + j) : 0.0f));
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR || P.splits > 1) cluster_sync_all();       // no CTA leaves while another may touch its shared memory or TMEM
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_free_all<PAIR>(tmem_base);
+    }
+}
+
+template <typename T>
+const void *variant(bool pair, bool bvec)
+{
+    if (pair) return bvec ? reinterpret_cast<const void *>(&fp8_gemm_kernel<true, true, T>) : reinterpret_cast<const void *>(&fp8_gemm_kernel<true, false, T>);
+    return bvec ? reinterpret_cast<const void *>(&fp8_gemm_kernel<false, true, T>) : reinterpret_cast<const void *>(&fp8_gemm_kernel<false, false, T>);
+}
+const void *variant(int type, bool pair, bool bvec)
+{
+    if (type == CDL_F32) return variant<float>(pair, bvec);
+    return type == CDL_BF16 ? variant<__nv_bfloat16>(pair, bvec) : variant<__half>(pair, bvec);
+}
+
+// out = bias (or 0) where the reduced dimension is empty
+template <typename T>
+__global__ void fill_bias_kernel(T *out, long long ldo, long long M, int N, const float *bias)
+{
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < M * N; i += (long long)gridDim.x * blockDim.x)
+        out[i / N * ldo + i % N] = from_f32<T>(bias != nullptr ? bias[i % N] : 0.0f);
+}
+
+}  // namespace
+}  // namespace cdl
+
+extern "C" size_t cdl_fp8_matmul_workspace_bytes(int32_t M, int32_t N, int32_t K)
+{
+    return M < 0 || N < 0 || K < 0 ? 0 : 256;           // the status block
+}
+
+extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, const void *B, int64_t ldb, const float *b_scale,
+                              int32_t b_mode, int32_t M, int32_t N, int32_t K, void *out, int64_t ldo, int32_t out_type,
+                              const float *bias, void *ws, size_t ws_bytes, void *stream)
+{
+    using namespace cdl;
+    if (M < 0 || N < 0 || K < 0 || !valid_type(out_type) || (b_mode != CDL_FP8_ROWS && b_mode != CDL_FP8_BLOCKS)) return CDL_ERR_ARG;
+    if (M == 0 || N == 0) return CDL_OK;
+    if (out == nullptr || ldo < N) return CDL_ERR_ARG;
+    if (K > 0 && (A == nullptr || B == nullptr || a_scale == nullptr || b_scale == nullptr || lda < K || ldb < K)) return CDL_ERR_ARG;
+    if (misaligned(out, out_type) || (reinterpret_cast<uintptr_t>(bias) & 3u)) return CDL_ERR_ALIGN;
+    if (K > 0 && ((reinterpret_cast<uintptr_t>(A) & 15u) || (reinterpret_cast<uintptr_t>(B) & 15u) || (lda & 15) || (ldb & 15) ||
+                  (reinterpret_cast<uintptr_t>(a_scale) & 3u) || (reinterpret_cast<uintptr_t>(b_scale) & 3u)))
+        return CDL_ERR_ALIGN;
+    if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255u) || ws_bytes < cdl_fp8_matmul_workspace_bytes(M, N, K)) return CDL_ERR_WORKSPACE;
+    int rc = check_device();
+    if (rc != CDL_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int sms = sm_count();
+    if (sms <= 0) return CDL_ERR_LAUNCH;
+    if (K == 0) {
+        if (out_type == CDL_F32) fill_bias_kernel<<<sms * 4, 256, 0, st>>>(static_cast<float *>(out), ldo, M, N, bias);
+        else if (out_type == CDL_BF16) fill_bias_kernel<<<sms * 4, 256, 0, st>>>(static_cast<__nv_bfloat16 *>(out), ldo, M, N, bias);
+        else fill_bias_kernel<<<sms * 4, 256, 0, st>>>(static_cast<__half *>(out), ldo, M, N, bias);
+        return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
+    }
+    Fp8Params P;
+    memset(&P, 0, sizeof P);
+    P.M = M;
+    P.N = N;
+    P.KB = (int)(((int64_t)K + 127) / 128);
+    const bool bvec = b_mode == CDL_FP8_ROWS;
+    P.nb = bvec ? N : (int)(((int64_t)N + 127) / 128);
+    P.sa = a_scale;
+    P.sb = b_scale;
+    P.bias = bias;
+    P.out = out;
+    P.ldo = ldo;
+    P.status = static_cast<int *>(ws);
+    const int64_t pair_tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
+    const int64_t tiles = (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128);
+    if (tiles > 0x3fffffff) return CDL_ERR_ARG;
+    const bool pair = pair_tiles >= sms / 2;
+    P.tiles_i = pair ? (M + 255) / 256 : (M + 127) / 128;
+    P.tiles_j = pair ? (N + 255) / 256 : (N + 127) / 128;
+    P.splits = 1;
+    if (!pair) {
+        int64_t s = sms / tiles;
+        if (s > P.KB / 2) s = P.KB / 2;
+        if (s > kMaxSplits) s = kMaxSplits;
+        while (P.splits * 2 <= s) P.splits *= 2;        // powers of two: they fill a GPC's SMs
+    }
+    const int esz = type_bytes(out_type);
+    // (a TMA store fills the last 16-byte unit of a row with zeros beyond N: rows that do not end on one are stored directly)
+    P.out_tma = P.splits == 1 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && (ldo * esz) % 16 == 0 && ((int64_t)N * esz) % 16 == 0;
+    CUtensorMap map_a, map_b, map_o;
+    bool ok = encode_map_2d(&map_a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, A, (uint64_t)K, (uint64_t)M, (uint64_t)lda, 128) &&
+              encode_map_2d(&map_b, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, B, (uint64_t)K, (uint64_t)N, (uint64_t)ldb, 128);
+    map_o = map_a;
+    if (P.out_tma)
+        ok = ok && encode_map_2d(&map_o, out_type == CDL_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                                             : (out_type == CDL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16),
+                                 esz, out, (uint64_t)N, (uint64_t)M, (uint64_t)(ldo * esz), 32);
+    if (!ok) return CDL_ERR_LAUNCH;
+    static bool attr_set[64];
+    static int pair_slots[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return CDL_ERR_LAUNCH;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.blockDim = dim3(kThreads);
+    cfg.attrs = at;
+    if (!attr_set[dev]) {
+        for (int t = 0; t < 3; ++t)
+            for (int v = 0; v < 4; ++v)
+                if (cudaFuncSetAttribute(variant(t, (v & 1) != 0, (v & 2) != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes((v & 2) != 0)) != cudaSuccess) {
+                    (void)cudaGetLastError();
+                    return CDL_ERR_LAUNCH;
+                }
+        // the pair kernels' shares must fit what a block is launched with, or an epilogue warpgroup would wait for good
+        for (int t = 0; t < 3; ++t)
+            for (int v = 0; v < 2; ++v) {
+                cudaFuncAttributes fa;
+                if (cudaFuncGetAttributes(&fa, variant(t, true, v != 0)) != cudaSuccess || fa.numRegs < kRegsLaunch) {
+                    (void)cudaGetLastError();
+                    return CDL_ERR_LAUNCH;
+                }
+            }
+        at[0].val.clusterDim.x = 2;
+        cfg.gridDim = dim3(2u * (unsigned)(sms / 2));
+        cfg.dynamicSmemBytes = smem_bytes(false);
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, variant(CDL_BF16, true, false), &cfg) != cudaSuccess || n < 1) {
+            (void)cudaGetLastError();
+            n = sms / 2;
+        }
+        pair_slots[dev] = n < sms / 2 ? n : sms / 2;
+        attr_set[dev] = true;
+    }
+    const int64_t units = (int64_t)P.tiles_i * P.tiles_j;
+    const int64_t dev_slots = pair ? pair_slots[dev] : (P.splits > 1 ? units : sms);
+    P.slots = (int)(units < dev_slots ? units : dev_slots);
+    at[0].val.clusterDim.x = pair ? 2u : (unsigned)P.splits;
+    cfg.gridDim = dim3((pair ? 2u : (unsigned)P.splits) * (unsigned)P.slots);
+    cfg.dynamicSmemBytes = smem_bytes(bvec);
+    cfg.stream = st;
+    cfg.numAttrs = pair || P.splits > 1 ? 1 : 0;
+    void *args[4] = {&map_a, &map_b, &map_o, &P};
+    if (cudaLaunchKernelExC(&cfg, variant(out_type, pair, bvec), args) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CDL_ERR_LAUNCH;
+    }
+    return CDL_OK;
+}

@@ -1,0 +1,223 @@
+// Block-scaled 8-bit floating-point quantizer: e4m3 codes with one binary32 scale per group of 128 consecutive entries
+// of a row (CDL_FP8_ROWS) or per 128 x 128 block (CDL_FP8_BLOCKS):
+//   s = max(RN(amax * RN(1/448)), 2^-126),   r = RN(1/s),   code = e4m3(sat(RN(x * r)))   (nearest even, saturated at 448)
+// and, from the same read of x, the codes and scales of the transposed matrix (row mode: with the transposed matrix's own
+// groups, 128 rows of a column).
+//
+// One CTA takes a 128 x 128 tile: every group of either orientation lies in one tile, so the tile is read once and kept in
+// registers between its maxima and its codes.  A thread holds 8 rows x 8 columns; the sixteen threads of a row own
+// 128 consecutive columns, so loads and code stores are whole lines, and a row's maximum is four shuffles.  The transposed
+// codes go through 16 KB of shared memory in units of 8 rows, the unit number exclusive-ored with the column's, which
+// keeps both the stores (a thread has eight rows of one column) and the loads (a warp writes two columns) free of bank
+// conflicts.  HBM is the bound: 4 (bf16, both orientations) to 6 (f32) bytes per element.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "cdl_internal.h"
+#include "cdl_lowp.cuh"
+
+namespace cdl {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kInvMax = 1.0f / 448.0f;
+constexpr float kTiny = 1.17549435e-38f;      // 2^-126
+
+struct QuantFp8 {
+    const void *x;
+    long long ldx;
+    int rows, cols;
+    int tiles_i, tiles_j;      // 128 x 128 tiles along the rows and the columns; one CTA each, columns fastest
+    unsigned char *codes, *codes_t;
+    long long ldc, ldt;
+    float *scales, *scales_t;
+};
+
+__device__ __forceinline__ void scale_of(float amax, float &s, float &r)
+{
+    s = fmaxf(__fmul_rn(amax, kInvMax), kTiny);
+    r = __frcp_rn(s);
+}
+
+// codes of two values, the first in the low byte (saturating; NaN becomes the NaN code)
+__device__ __forceinline__ uint32_t code2(float a, float b)
+{
+    uint16_t w;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(w) : "f"(b), "f"(a));
+    return w;
+}
+
+// BLOCKS: one scale for the tile; otherwise one per row of the tile and, with BOTH, one per column.  VEC: rows of x can be
+// read 16 bytes at a time.
+template <typename T, bool BLOCKS, bool BOTH, bool VEC>
+__global__ void __launch_bounds__(kThreads, 2)
+quantize_fp8_kernel(const QuantFp8 Q)
+{
+    __shared__ float part[8][128];                              // per warp: column maxima, or one tile maximum
+    __shared__ __align__(16) unsigned char tile_t[BOTH ? 128 * 128 : 16];
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int ti = (int)(blockIdx.x / (unsigned)Q.tiles_j), tj = (int)(blockIdx.x - (unsigned)ti * (unsigned)Q.tiles_j);
+    const int r0 = ti * 128, c0 = tj * 128;
+    const int row = r0 + ty * 8, col = c0 + tx * 8;             // this thread's 8 x 8 piece
+    const T *x = static_cast<const T *>(Q.x);
+
+    float v[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const T *p = x + (long long)(row + i) * Q.ldx + col;
+        if (row + i < Q.rows && col + 8 <= Q.cols && VEC) {
+            load8(p, v[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = row + i < Q.rows && col + j < Q.cols ? to_f32(p[j]) : 0.0f;
+        }
+    }
+    // maxima of magnitudes (fmaxf drops a NaN: it does not enter a group's scale)
+    float rmax[8], cmax[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        rmax[i] = 0.0f;
+        if (i == 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) cmax[j] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            rmax[i] = fmaxf(rmax[i], fabsf(v[i][j]));
+            if (BOTH && !BLOCKS) cmax[j] = fmaxf(cmax[j], fabsf(v[i][j]));
+        }
+    }
+    float rrec[8], crec[8];
+    if (BLOCKS) {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, rmax[i]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) part[warp][0] = m;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, part[k][0]);
+        float s, r;
+        scale_of(m, s, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rrec[i] = crec[i] = r;
+        if (threadIdx.x == 0) {
+            Q.scales[(long long)tj * Q.tiles_i + ti] = s;
+            if (BOTH) Q.scales_t[(long long)ti * Q.tiles_j + tj] = s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) rmax[i] = fmaxf(rmax[i], __shfl_xor_sync(0xffffffffu, rmax[i], o));
+            float s;
+            scale_of(rmax[i], s, rrec[i]);
+            if (tx == i && row + i < Q.rows) Q.scales[(long long)tj * Q.rows + row + i] = s;
+        }
+        if (BOTH) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) cmax[j] = fmaxf(cmax[j], __shfl_xor_sync(0xffffffffu, cmax[j], 16));
+            if (lane < 16) {
+                *reinterpret_cast<float4 *>(&part[warp][tx * 8]) = make_float4(cmax[0], cmax[1], cmax[2], cmax[3]);
+                *reinterpret_cast<float4 *>(&part[warp][tx * 8 + 4]) = make_float4(cmax[4], cmax[5], cmax[6], cmax[7]);
+            }
+            __syncthreads();
+            if (threadIdx.x < 128) {        // one column each; the reciprocal goes back through part[0]
+                float m = part[0][threadIdx.x];
+#pragma unroll
+                for (int k = 1; k < 8; ++k) m = fmaxf(m, part[k][threadIdx.x]);
+                float s, r;
+                scale_of(m, s, r);
+                part[0][threadIdx.x] = r;
+                if (c0 + (int)threadIdx.x < Q.cols) Q.scales_t[(long long)ti * Q.cols + c0 + threadIdx.x] = s;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) crec[j] = part[0][tx * 8 + j];
+        }
+    }
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (row + i >= Q.rows || col >= Q.cols) continue;
+            uint32_t h[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[j] = code2(__fmul_rn(v[i][2 * j], rrec[i]), __fmul_rn(v[i][2 * j + 1], rrec[i]));
+            unsigned char *p = Q.codes + (long long)(row + i) * Q.ldc + col;
+            if (col + 8 <= Q.cols) *reinterpret_cast<uint2 *>(p) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < Q.cols) p[j] = (unsigned char)(h[j >> 1] >> (8 * (j & 1)));
+        }
+    }
+    if (BOTH) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = code2(__fmul_rn(v[2 * i][j], crec[j]), __fmul_rn(v[2 * i + 1][j], crec[j]));
+            *reinterpret_cast<uint2 *>(&tile_t[(tx * 8 + j) * 128 + ((ty ^ tx) << 3)]) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int c = k * 16 + ty, unit = tx;                // sixteen threads write the 128 rows of one column
+            if (c0 + c >= Q.cols) continue;
+            const uint2 w = *reinterpret_cast<const uint2 *>(&tile_t[c * 128 + ((unit ^ (c >> 3)) << 3)]);
+            const int rr = r0 + unit * 8;
+            unsigned char *p = Q.codes_t + (long long)(c0 + c) * Q.ldt + rr;
+            if (rr + 8 <= Q.rows) *reinterpret_cast<uint2 *>(p) = w;
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (rr + j < Q.rows) p[j] = (unsigned char)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+        }
+    }
+}
+
+template <typename T>
+int launch_typed(const QuantFp8 &Q, bool blocks, cudaStream_t stream)
+{
+    const bool vec = (reinterpret_cast<uintptr_t>(Q.x) & 15u) == 0 && (Q.rows == 1 || (Q.ldx * (long long)sizeof(T)) % 16 == 0);
+    const unsigned grid = (unsigned)Q.tiles_i * (unsigned)Q.tiles_j;
+    const bool both = Q.codes_t != nullptr;
+#define CDL_GO(BL, BO, VE) quantize_fp8_kernel<T, BL, BO, VE><<<grid, kThreads, 0, stream>>>(Q)
+    if (vec) {
+        if (blocks) { if (both) CDL_GO(true, true, true); else CDL_GO(true, false, true); }
+        else { if (both) CDL_GO(false, true, true); else CDL_GO(false, false, true); }
+    } else {
+        if (blocks) { if (both) CDL_GO(true, true, false); else CDL_GO(true, false, false); }
+        else { if (both) CDL_GO(false, true, false); else CDL_GO(false, false, false); }
+    }
+#undef CDL_GO
+    return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
+}
+
+}  // namespace
+}  // namespace cdl
+
+extern "C" int cdl_fp8_quantize(const void *x, int64_t ldx, int32_t type, int32_t rows, int32_t cols, int32_t mode, void *codes,
+                                int64_t ldc, float *scales, void *codes_t, int64_t ldt, float *scales_t, void *stream)
+{
+    using namespace cdl;
+    if (rows < 0 || cols < 0 || !valid_type(type) || (mode != CDL_FP8_ROWS && mode != CDL_FP8_BLOCKS)) return CDL_ERR_ARG;
+    if (rows == 0 || cols == 0) return CDL_OK;
+    if (x == nullptr || codes == nullptr || scales == nullptr || (codes_t == nullptr) != (scales_t == nullptr)) return CDL_ERR_ARG;
+    if ((rows > 1 && ldx < cols) || ldc < cols || (codes_t != nullptr && ldt < rows)) return CDL_ERR_ARG;
+    const int64_t tiles_i = ((int64_t)rows + 127) / 128, tiles_j = ((int64_t)cols + 127) / 128;
+    if (tiles_i * tiles_j > 0x7fffffff) return CDL_ERR_ARG;
+    if (misaligned(x, type) || (reinterpret_cast<uintptr_t>(scales) & 3u) || (reinterpret_cast<uintptr_t>(scales_t) & 3u)) return CDL_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(codes) & 15u) || (ldc & 15) || (reinterpret_cast<uintptr_t>(codes_t) & 15u) || (codes_t != nullptr && (ldt & 15)))
+        return CDL_ERR_ALIGN;
+    int rc = check_device();
+    if (rc != CDL_OK) return rc;
+    const QuantFp8 Q{x, ldx, rows, cols, (int)tiles_i, (int)tiles_j, static_cast<unsigned char *>(codes), static_cast<unsigned char *>(codes_t), ldc, ldt, scales, scales_t};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool blocks = mode == CDL_FP8_BLOCKS;
+    switch (type) {
+    case CDL_F32: return launch_typed<float>(Q, blocks, st);
+    case CDL_BF16: return launch_typed<__nv_bfloat16>(Q, blocks, st);
+    default: return launch_typed<__half>(Q, blocks, st);
+    }
+}
