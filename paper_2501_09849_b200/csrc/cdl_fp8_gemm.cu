@@ -27,7 +27,7 @@ namespace cdl {
 namespace {
 
 constexpr int kEpiWarps = 8;
-constexpr int kThreads = 128 + 32 * kEpiWarps;         // a warpgroup of which two warps drive the pipeline, two of epilogue warps
+constexpr int kThreads = 128 + 32 * kEpiWarps;         // a warpgroup whose first three warps feed the others, two of epilogue warps
 // Registers: a pair's epilogue thread holds 128 sums besides the 32 partial ones it has just read, more than an even share
 // of the register file (168 for 384 threads).  The first warpgroup gives up what it does not need:
 // 128 * 88 + 256 * 208 = 384 * 168.
@@ -35,15 +35,20 @@ constexpr int kRegsLaunch = 168, kRegsDrive = 88, kRegsEpilogue = 208;
 static_assert(128 * kRegsDrive + 32 * kEpiWarps * kRegsEpilogue <= kThreads * kRegsLaunch, "register shares");
 constexpr int kBlockBytes = 128 * 128;                 // one operand block of a stage: 128 rows x 128 bytes
 constexpr int kStageBytes = 2 * kBlockBytes;
-constexpr int kOutWarpBytes = 32 * 128;                // output staging of one epilogue warp
+constexpr int kOutBytes = 32 * 64;                     // output staging block of a warp: 32 rows x 64 bytes
+constexpr int kOutBlocks = 2;                          // ... of which a warp has as many stores in flight
+constexpr int kOutWarpBytes = kOutBlocks * kOutBytes;
 constexpr int kStagesMax = 6;
-__host__ __device__ constexpr int stages(bool bvec) { return bvec ? 5 : 6; }
+constexpr int kGroup = 4;                              // stages whose scales are handed over together
+constexpr int kScaleSlots = 4;                         // groups on their way or in use
+__host__ __device__ constexpr int stages(bool bvec) { return bvec ? 5 : 5; }
+__host__ __device__ constexpr int slot_floats(bool bvec) { return bvec ? 128 + 256 : 128 + 4; }      // scales of a stage: rows, then columns
 __host__ __device__ constexpr int smem_bytes(bool bvec)
 {
-    return 1024 + stages(bvec) * kStageBytes + kEpiWarps * kOutWarpBytes + (bvec ? kEpiWarps * 2 * 128 * 4 : 0);
+    return 1024 + stages(bvec) * kStageBytes + kEpiWarps * kOutWarpBytes + kScaleSlots * kGroup * slot_floats(bvec) * 4;
 }
-constexpr int kMaxSplits = 8;                          // portable cluster size
 constexpr unsigned long long kWaitNs = 2000000000ull;
+constexpr int kMaxSplits = 8;                          // portable cluster size
 
 struct Fp8Params {
     int M, N, KB;                   // KB: blocks of 128 along the reduced dimension
@@ -56,6 +61,24 @@ struct Fp8Params {
     int out_tma;                    // the output goes through shared memory and TMA
     int *status;
 };
+
+// four bytes from global to shared memory, asynchronously; zero where `live` is not set (nothing is read then)
+__device__ __forceinline__ void copy4_async(uint32_t dst, const float *src, bool live)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ float lds32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 lds128(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 
 // Tiles in bands of eight tile rows, columns outer, so that what runs at one time shares operand blocks in L2.
 __device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti, int &tj)
@@ -72,13 +95,13 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const __grid_constant__ CUtensorMap map_o, const Fp8Params P)
 {
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 8];
+    __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 8 + 2 * kScaleSlots];
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s;
 
     constexpr int kStages = stages(BVEC);
-    constexpr int kBufs = PAIR ? 2 : 4;                // TMEM buffers of a partial tile
     constexpr int kTN = PAIR ? 256 : 128;
+    constexpr int kBufs = 512 / kTN;                   // TMEM buffers of a partial tile
     constexpr int kCols = kTN / 2;                     // columns of an epilogue warp
     const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -92,7 +115,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 
     const uint32_t bar0 = smem_u32(&bars[0]);
     constexpr uint32_t kEmptyOff = 8u * kStagesMax;
-    const uint32_t tfull0 = bar0 + 16u * kStagesMax, tempty0 = tfull0 + 8u * kBufs;
+    const uint32_t tfull0 = bar0 + 16u * kStagesMax, tempty0 = tfull0 + 32u;
+    const uint32_t sfull0 = tempty0 + 32u;              // scales of a stage are there; taken: + 8 kScaleSlots
     if (threadIdx.x == 0) {
         abort_s = 0;
         for (int s = 0; s < kStages; ++s) {
@@ -101,7 +125,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
         for (int b = 0; b < kBufs; ++b) {
             mbar_init(tfull0 + 8u * b, 1);
-            mbar_init(tempty0 + 8u * b, PAIR ? 2 * kEpiWarps : kEpiWarps);
+            mbar_init(tempty0 + 8u * b, (PAIR ? 2 : 1) * kEpiWarps);
+        }
+        for (int s = 0; s < kScaleSlots; ++s) {
+            mbar_init(sfull0 + 8u * s, 32);
+            mbar_init(sfull0 + 8u * (kScaleSlots + s), kEpiWarps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -112,6 +140,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_s;
     bool failed = false;
+    const uint32_t scale_base = smem_base + (uint32_t)(kStages * kStageBytes + kEpiWarps * kOutWarpBytes);
 
     if (warp < 4) {
         if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsDrive));
@@ -156,9 +185,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 uint32_t st = 0u, par = 0u, buf = 0u, tpar = 1u;
                 for (int u = slot; u < units && !failed; u += P.slots) {
                     for (int kb = kb0; kb < kb1; ++kb) {
-                        const uint32_t fb = bar0 + 8u * st;
-                        if ((!mbar_try_wait_now(tempty0 + 8u * buf, tpar) && !mbar_wait(tempty0 + 8u * buf, tpar, abort_flag, kWaitNs)) ||
-                            (!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs))) {
+                        const uint32_t fb = bar0 + 8u * st, tf = tfull0 + 8u * buf, te = tempty0 + 8u * buf;
+                        if ((!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs)) ||
+                            (!mbar_try_wait_now(te, tpar) && !mbar_wait(te, tpar, abort_flag, kWaitNs))) {
                             failed = true;
                             break;
                         }
@@ -166,11 +195,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         const uint32_t off = st * (uint32_t)(kStageBytes >> 4);
                         tc_mma4<PAIR, KIND_F8F6F4>(tmem_base + buf * (uint32_t)kTN, a_lo0 + off, a_hi, 2u, b_lo0 + off, b_hi, 2u, idesc, 0u);
                         if (PAIR) {
+                            tc_commit_pair(tf);
                             tc_commit_pair(fb + kEmptyOff);
-                            tc_commit_pair(tfull0 + 8u * buf);
                         } else {
+                            tc_commit(tf);
                             tc_commit(fb + kEmptyOff);
-                            tc_commit(tfull0 + 8u * buf);
                         }
                         if (++st == (uint32_t)kStages) {
                             st = 0u;
@@ -183,87 +212,139 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                 }
             }
+        } else if (warp == 2) {
+            // ------------------------------------------------------------ scales: a stage's row and column scales by
+            // asynchronous 4-byte copies (their addresses have no alignment to rely on), several stages ahead
+            uint32_t q = 0u, par = 1u;
+            for (int u = slot; u < units && !failed; u += P.slots) {
+                int ti, tj;
+                tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+                const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0), col = tj * kTN;
+                for (int kg = kb0; kg < kb1; kg += kGroup) {
+                    const uint32_t sf = sfull0 + 8u * q;
+                    if (!__all_sync(0xffffffffu, mbar_try_wait_now(sf + 8u * kScaleSlots, par) || mbar_wait(sf + 8u * kScaleSlots, par, abort_flag, kWaitNs))) {
+                        failed = true;
+                        break;
+                    }
+                    for (int kb = kg; kb < min(kg + kGroup, kb1); ++kb) {
+                        const uint32_t dst = scale_base + (q * (uint32_t)kGroup + (uint32_t)(kb - kg)) * (uint32_t)(slot_floats(BVEC) * 4);
+                        const float *pa = P.sa + (long long)kb * P.M, *pb = P.sb + (long long)kb * P.nb;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = arow + i * 32 + lane;
+                            copy4_async(dst + (uint32_t)(i * 32 + lane) * 4u, r < P.M ? pa + r : P.sa, r < P.M);
+                        }
+                        if (BVEC) {
+#pragma unroll
+                            for (int i = 0; i < kTN / 32; ++i) {
+                                const int c = col + i * 32 + lane;
+                                copy4_async(dst + (uint32_t)(128 + i * 32 + lane) * 4u, c < P.N ? pb + c : P.sb, c < P.N);
+                            }
+                        } else if (lane < kTN / 128) {
+                            const int c = (col >> 7) + lane;
+                            copy4_async(dst + (uint32_t)(128 + lane) * 4u, c < P.nb ? pb + c : P.sb, c < P.nb);
+                        }
+                    }
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(sf) : "memory");
+                    if (++q == (uint32_t)kScaleSlots) {
+                        q = 0u;
+                        par ^= 1u;
+                    }
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
         }
     } else {
         if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
-        // ------------------------------------------------------------ epilogue warps
+        // ------------------------------------------------------------ epilogue warps: 32 rows x kCols columns each
         float2 acc[kCols / 2];
-        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const int quarter = warp & 3, group = (warp - 4) >> 2;
+        auto tile_col = [&](int ch) { return group * kCols + ch * 32; };      // of chunk ch of 32 columns
         const uint32_t wbuf = smem_base + (uint32_t)(kStages * kStageBytes) + (uint32_t)((warp - 4) * kOutWarpBytes);
-        float *sbuf = reinterpret_cast<float *>(smem_dyn + (smem_base - smem_u32(smem_dyn)) + kStages * kStageBytes + kEpiWarps * kOutWarpBytes) +
-                      (warp - 4) * 256;
-        uint32_t buf = 0u, tpar = 0u;
-        constexpr int kLaneCols = kCols / 32;           // column scales a lane fetches per stage (BVEC)
+        uint32_t buf = 0u, tpar = 0u, q = 0u, spar = 0u, oblk = 0u;
         for (int u = slot; u < units && !failed; u += P.slots) {
             int ti, tj;
             tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
             const int row0 = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
-            const int col0 = tj * kTN + half * kCols;
             const int row = row0 + lane;
-            // scales two stages ahead of their use
-            auto load_sa = [&](int kb) { return row < P.M && kb < kb1 ? __ldg(P.sa + (long long)kb * P.M + row) : 0.0f; };
-            auto load_sb = [&](int kb, float (&s)[4]) {
-                if (BVEC) {
-#pragma unroll
-                    for (int j = 0; j < kLaneCols; ++j) {
-                        const int c = col0 + lane * kLaneCols + j;
-                        s[j] = c < P.N && kb < kb1 ? __ldg(P.sb + (long long)kb * P.N + c) : 0.0f;
-                    }
-                } else {
-                    s[0] = col0 < P.N && kb < kb1 ? __ldg(P.sb + (long long)kb * P.nb + (col0 >> 7)) : 0.0f;
-                }
-            };
-            float sa0 = load_sa(kb0), sa1 = load_sa(kb0 + 1);
-            float sb0[4], sb1[4];
-            load_sb(kb0, sb0);
-            load_sb(kb0 + 1, sb1);
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
-            if (BVEC) __syncwarp();                      // the last tile's column scales have been read
+            int in = 0;                                  // stage of the group
             for (int kb = kb0; kb < kb1; ++kb) {
-                const float sa = sa0;
-                const float s_row = BVEC ? sa : sa * sb0[0];
-                float *sv = sbuf + (kb & 1) * 128;
-                if (BVEC) {
-                    if (kLaneCols == 4) *reinterpret_cast<float4 *>(sv + lane * 4) = make_float4(sb0[0], sb0[1], sb0[2], sb0[3]);
-                    else *reinterpret_cast<float2 *>(sv + lane * 2) = make_float2(sb0[0], sb0[1]);
-                    __syncwarp();
+                const uint32_t blk = buf, tf = tfull0 + 8u * blk;
+                if (in == 0) {
+                    const uint32_t sf = sfull0 + 8u * q;
+                    if (!__all_sync(0xffffffffu, mbar_try_wait_now(sf, spar) || mbar_wait(sf, spar, abort_flag, kWaitNs))) {
+                        failed = true;
+                        break;
+                    }
                 }
-                sa0 = sa1;
-                sa1 = load_sa(kb + 2);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sb0[j] = sb1[j];
-                load_sb(kb + 2, sb1);
-                const uint32_t tf = tfull0 + 8u * buf;
+                const uint32_t sc = scale_base + (q * (uint32_t)kGroup + (uint32_t)in) * (uint32_t)(slot_floats(BVEC) * 4);
+                float s_row = lds32(sc + (uint32_t)(quarter * 32 + lane) * 4u);
+                if (!BVEC) s_row *= lds32(sc + (uint32_t)(128 + (PAIR ? group : 0)) * 4u);
                 if (!__all_sync(0xffffffffu, mbar_try_wait_now(tf, tpar) || mbar_wait(tf, tpar, abort_flag, kWaitNs))) {
                     failed = true;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * (uint32_t)kTN + (uint32_t)(half * kCols);
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + blk * (uint32_t)kTN;
+                // 16 columns at a time, the next ones on their way while these are added
+                uint32_t va[16], vb[16];
+                float4 f[BVEC ? 4 : 1];                  // column scales of the 16 columns
+                auto fetch = [&](int c16) {
+                    if (BVEC) {
+                        const uint32_t sv = sc + (uint32_t)(128 + tile_col(c16 >> 1) + (c16 & 1) * 16) * 4u;
 #pragma unroll
-                for (int ch = 0; ch < kCols / 32; ++ch) {
-                    uint32_t v[32];
-                    tc_ld32(taddr + (uint32_t)(ch * 32), v);
-                    tc_wait_ld_pin(v);
-                    if (ch == kCols / 32 - 1) {          // the partial tile is in registers: its buffer is free
+                        for (int j = 0; j < 4; ++j) f[BVEC ? j : 0] = lds128(sv + (uint32_t)j * 16u);
+                    }
+                };
+                auto add = [&](const uint32_t (&v)[16], int c16) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float2 f0 = make_float2(s_row, s_row), f1 = f0;
+                        if (BVEC) {
+                            f0 = mul2(f0, make_float2(f[BVEC ? j : 0].x, f[BVEC ? j : 0].y));
+                            f1 = mul2(f1, make_float2(f[BVEC ? j : 0].z, f[BVEC ? j : 0].w));
+                        }
+                        fma2(acc[c16 * 8 + 2 * j], v[4 * j], v[4 * j + 1], f0);
+                        fma2(acc[c16 * 8 + 2 * j + 1], v[4 * j + 2], v[4 * j + 3], f1);
+                    }
+                };
+                tc_ld16(taddr + (uint32_t)tile_col(0), va);
+                fetch(0);
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    tc_wait_ld_pin(va);
+                    tc_ld16(taddr + (uint32_t)tile_col(c) + 16u, vb);
+                    add(va, 2 * c);
+                    fetch(2 * c + 1);
+                    tc_wait_ld_pin(vb);
+                    if (c < kCols / 32 - 1) {
+                        tc_ld16(taddr + (uint32_t)tile_col(c + 1), va);
+                        add(vb, 2 * c + 1);
+                        fetch(2 * c + 2);
+                    } else {                             // the partial tile is in registers: its buffer is free
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) {
-                            if (PAIR) mbar_arrive_remote(tempty0 + 8u * buf, 0u);
-                            else mbar_arrive(tempty0 + 8u * buf);
+                            if (PAIR) mbar_arrive_remote(tempty0 + 8u * blk, 0u);
+                            else mbar_arrive(tempty0 + 8u * blk);
+                        }
+                        if (++buf == (uint32_t)kBufs) {
+                            buf = 0u;
+                            tpar ^= 1u;
+                        }
+                        add(vb, 2 * c + 1);
+                        if (++in == kGroup || kb + 1 == kb1) {       // the group's scales have been read
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(sfull0 + 8u * (kScaleSlots + q));
+                            in = 0;
+                            if (++q == (uint32_t)kScaleSlots) {
+                                q = 0u;
+                                spar ^= 1u;
+                            }
                         }
                     }
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float2 s = make_float2(s_row, s_row);
-                        if (BVEC) s = mul2(s, *reinterpret_cast<const float2 *>(sv + ch * 32 + 2 * j));
-                        fma2(acc[ch * 16 + j], v[2 * j], v[2 * j + 1], s);
-                    }
-                }
-                if (++buf == (uint32_t)kBufs) {
-                    buf = 0u;
-                    tpar ^= 1u;
                 }
             }
             if (failed) break;
@@ -276,60 +357,62 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 if (row < P.M) {
 #pragma unroll
                     for (int j = 0; j < kCols / 4; ++j) {
-                        const int unit = half * (kCols / 4) + j;
+                        const int unit = (group * kCols >> 2) + j;
                         *reinterpret_cast<float4 *>(part + r * 128 + ((unit ^ (r & 7)) << 2)) =
                             make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
                     }
                 }
                 break;
             }
-            if (row0 >= P.M || col0 >= P.N) continue;
-            if (P.bias != nullptr) {
+            if (row0 >= P.M) continue;
 #pragma unroll
-                for (int j = 0; j < kCols / 2; ++j) {
-                    if (col0 + 2 * j < P.N) acc[j].x += __ldg(P.bias + col0 + 2 * j);
-                    if (col0 + 2 * j + 1 < P.N) acc[j].y += __ldg(P.bias + col0 + 2 * j + 1);
+            for (int ch = 0; ch < kCols / 32; ++ch) {
+                const int col0 = tj * kTN + tile_col(ch);
+                if (col0 >= P.N) continue;
+                float2 *a = acc + ch * 16;
+                if (P.bias != nullptr) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        if (col0 + 2 * j < P.N) a[j].x += __ldg(P.bias + col0 + 2 * j);
+                        if (col0 + 2 * j + 1 < P.N) a[j].y += __ldg(P.bias + col0 + 2 * j + 1);
+                    }
                 }
-            }
-            if (P.out_tma) {
-                // 128-byte pieces of the warp's 32 rows through its staging block: TMA clips at the edges
-                constexpr int kPiece = 128 / (int)sizeof(T);
+                if (P.out_tma) {
+                    // 64-byte pieces of the warp's 32 rows through its staging block (64-byte swizzle): TMA clips at the edges
+                    constexpr int kPiece = 64 / (int)sizeof(T);
 #pragma unroll
-                for (int pc = 0; pc < kCols / kPiece; ++pc) {
-                    if (col0 + pc * kPiece >= P.N) break;
-                    if (lane == 0) bulk_wait_read<0>();
-                    __syncwarp();
-                    const uint32_t dst = wbuf + (uint32_t)lane * 128u;
+                    for (int pc = 0; pc < 32 / kPiece; ++pc) {
+                        if (col0 + pc * kPiece >= P.N) break;
+                        if (lane == 0) bulk_wait_read<kOutBlocks - 1>();     // the store that last used this block has read it
+                        __syncwarp();
+                        const uint32_t src = wbuf + oblk, dst = src + (uint32_t)lane * 64u;
 #pragma unroll
-                    for (int c4 = 0; c4 < 8; ++c4) {
-                        uint32_t w[4];
+                        for (int c4 = 0; c4 < 4; ++c4) {
+                            uint32_t w[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if constexpr (sizeof(T) == 4) {
-                                const float2 a = acc[(pc * 32 + c4 * 4 + j) / 2];
-                                w[j] = __float_as_uint((j & 1) ? a.y : a.x);
-                            } else {
-                                const float2 a = acc[pc * 32 + c4 * 4 + j];
-                                w[j] = pack2<T>(a.x, a.y);
+                            for (int j = 0; j < 4; ++j) {
+                                if constexpr (sizeof(T) == 4) w[j] = __float_as_uint((j & 1) ? a[pc * 8 + c4 * 2 + (j >> 1)].y : a[pc * 8 + c4 * 2 + (j >> 1)].x);
+                                else w[j] = pack2<T>(a[c4 * 4 + j].x, a[c4 * 4 + j].y);
                             }
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c4 ^ ((lane >> 1) & 3)) << 4)),
+                                         "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                                         : "memory");
                         }
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c4 ^ (lane & 7)) << 4)),
-                                     "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                                     : "memory");
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&map_o, col0 + pc * kPiece, row0, src);
+                            bulk_commit();
+                        }
+                        oblk = oblk + (uint32_t)kOutBytes == (uint32_t)kOutWarpBytes ? 0u : oblk + (uint32_t)kOutBytes;
                     }
-                    fence_async_smem();
-                    __syncwarp();
-                    if (lane == 0) {
-                        tma_store_2d(&map_o, col0 + pc * kPiece, row0, wbuf);
-                        bulk_commit();
-                    }
-                }
-            } else if (row < P.M) {
-                T *o = static_cast<T *>(P.out) + (long long)row * P.ldo + col0;
+                } else if (row < P.M) {
+                    T *o = static_cast<T *>(P.out) + (long long)row * P.ldo + col0;
 #pragma unroll
-                for (int j = 0; j < kCols / 2; ++j) {
-                    if (col0 + 2 * j < P.N) o[2 * j] = from_f32<T>(acc[j].x);
-                    if (col0 + 2 * j + 1 < P.N) o[2 * j + 1] = from_f32<T>(acc[j].y);
+                    for (int j = 0; j < 16; ++j) {
+                        if (col0 + 2 * j < P.N) o[2 * j] = from_f32<T>(a[j].x);
+                        if (col0 + 2 * j + 1 < P.N) o[2 * j + 1] = from_f32<T>(a[j].y);
+                    }
                 }
             }
         }
@@ -470,7 +553,7 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     if (P.out_tma)
         ok = ok && encode_map_2d(&map_o, out_type == CDL_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                                              : (out_type == CDL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16),
-                                 esz, out, (uint64_t)N, (uint64_t)M, (uint64_t)(ldo * esz), 32);
+                                 esz, out, (uint64_t)N, (uint64_t)M, (uint64_t)(ldo * esz), 32, 64);
     if (!ok) return CDL_ERR_LAUNCH;
     static bool attr_set[64];
     static int pair_slots[64];

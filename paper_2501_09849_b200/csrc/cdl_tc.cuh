@@ -107,6 +107,21 @@ __device__ __forceinline__ void tc_wait_ld_pin(uint32_t (&v)[32])
                  : "memory");
 }
 
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld_pin(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+
 // Shared-memory operand descriptor (sm_100 format): start address, leading / stride byte offsets in 16-byte
 // units, version 1, 128-byte swizzle.
 __device__ __forceinline__ uint64_t make_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes)
@@ -217,19 +232,20 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
     return c;
 }
 
-// Two-dimensional tensor map of `cols` x `rows` elements (cols contiguous, row pitch in bytes) with boxes 128 bytes wide
-// under the 128-byte swizzle; reads outside are zero, writes outside are dropped.
+// Two-dimensional tensor map of `cols` x `rows` elements (cols contiguous, row pitch in bytes) with boxes of 128 (or 64)
+// bytes under the swizzle of that width; reads outside are zero, writes outside are dropped in units of 16 bytes.
 inline bool encode_map_2d(CUtensorMap *map, CUtensorMapDataType type, int elem_bytes, const void *base, uint64_t cols, uint64_t rows,
-                          uint64_t pitch_bytes, uint32_t box_rows)
+                          uint64_t pitch_bytes, uint32_t box_rows, uint32_t box_bytes = 128)
 {
     EncodeTiledFn fn = get_encode();
     if (fn == nullptr) return false;
     const cuuint64_t dims[2] = {cols, rows};
     const cuuint64_t strides[1] = {pitch_bytes};
-    const cuuint32_t box[2] = {128u / (uint32_t)elem_bytes, box_rows};
+    const cuuint32_t box[2] = {box_bytes / (uint32_t)elem_bytes, box_rows};
     const cuuint32_t estr[2] = {1u, 1u};
-    return fn(map, type, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, type, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace cdl
