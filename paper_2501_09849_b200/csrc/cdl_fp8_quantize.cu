@@ -47,13 +47,112 @@ __device__ __forceinline__ uint32_t code2(float a, float b)
     return w;
 }
 
+// A thread's 8 x 8 piece of the tile: 64 floats, or 32 words of two 16-bit values, whose magnitudes are compared two at a
+// time.  Maxima drop a NaN: it does not enter a group's scale.
+template <typename T>
+struct Piece {
+    uint32_t w[8][4];
+    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
+    {
+        uint32_t m;
+        if (__is_same(T, __nv_bfloat16)) asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+        else asm("max.f16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+        return m;
+    }
+    static __device__ __forceinline__ float max_of(uint32_t m)
+    {
+        float lo, hi;
+        unpack2(m, lo, hi, T());
+        return fmaxf(lo, hi);
+    }
+    __device__ __forceinline__ void load(int i, const T *p)
+    {
+        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(p));
+        w[i][0] = q.x;
+        w[i][1] = q.y;
+        w[i][2] = q.z;
+        w[i][3] = q.w;
+    }
+    __device__ __forceinline__ void load_some(int i, const T *p, int live)
+    {
+        const unsigned short *h = reinterpret_cast<const unsigned short *>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[i][j] = (2 * j < live ? (uint32_t)h[2 * j] : 0u) | (2 * j + 1 < live ? (uint32_t)h[2 * j + 1] << 16 : 0u);
+    }
+    __device__ __forceinline__ float row_max(int i) const
+    {
+        const uint32_t k = 0x7fff7fffu;
+        return max_of(max2(max2(w[i][0] & k, w[i][1] & k), max2(w[i][2] & k, w[i][3] & k)));
+    }
+    // maxima of the 8 columns over the warp's 16 rows -> part (floats)
+    __device__ __forceinline__ void column_max(float *part, int lane) const
+    {
+        const uint32_t k = 0x7fff7fffu;
+        float c[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t m = w[0][j] & k;
+#pragma unroll
+            for (int i = 1; i < 8; ++i) m = max2(m, w[i][j] & k);
+            m = max2(m, __shfl_xor_sync(0xffffffffu, m, 16));
+            unpack2(m, c[2 * j], c[2 * j + 1], T());
+            c[2 * j] = fmaxf(c[2 * j], 0.0f);            // (both NaN: no magnitude)
+            c[2 * j + 1] = fmaxf(c[2 * j + 1], 0.0f);
+        }
+        if (lane < 16) {
+            *reinterpret_cast<float4 *>(part) = make_float4(c[0], c[1], c[2], c[3]);
+            *reinterpret_cast<float4 *>(part + 4) = make_float4(c[4], c[5], c[6], c[7]);
+        }
+    }
+    __device__ __forceinline__ float value(int i, int j) const
+    {
+        float lo, hi;
+        unpack2(w[i][j >> 1], lo, hi, T());
+        return (j & 1) ? hi : lo;
+    }
+};
+template <>
+struct Piece<float> {
+    float v[8][8];
+    __device__ __forceinline__ void load(int i, const float *p) { load8(p, v[i]); }
+    __device__ __forceinline__ void load_some(int i, const float *p, int live)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = j < live ? p[j] : 0.0f;
+    }
+    __device__ __forceinline__ float row_max(int i) const
+    {
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
+        return m;
+    }
+    __device__ __forceinline__ void column_max(float *part, int lane) const
+    {
+        float c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            c[j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[j] = fmaxf(c[j], fabsf(v[i][j]));
+            c[j] = fmaxf(c[j], __shfl_xor_sync(0xffffffffu, c[j], 16));
+        }
+        if (lane < 16) {
+            *reinterpret_cast<float4 *>(part) = make_float4(c[0], c[1], c[2], c[3]);
+            *reinterpret_cast<float4 *>(part + 4) = make_float4(c[4], c[5], c[6], c[7]);
+        }
+    }
+    __device__ __forceinline__ float value(int i, int j) const { return v[i][j]; }
+};
+
 // BLOCKS: one scale for the tile; otherwise one per row of the tile and, with BOTH, one per column.  VEC: rows of x can be
 // read 16 bytes at a time.
 template <typename T, bool BLOCKS, bool BOTH, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 4)
 quantize_fp8_kernel(const QuantFp8 Q)
 {
-    __shared__ float part[8][128];                              // per warp: column maxima, or one tile maximum
+    __shared__ __align__(16) float part[8][128];                // per warp: column maxima, or one tile maximum
     __shared__ __align__(16) unsigned char tile_t[BOTH ? 128 * 128 : 16];
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ti = (int)(blockIdx.x / (unsigned)Q.tiles_j), tj = (int)(blockIdx.x - (unsigned)ti * (unsigned)Q.tiles_j);
@@ -61,36 +160,23 @@ quantize_fp8_kernel(const QuantFp8 Q)
     const int row = r0 + ty * 8, col = c0 + tx * 8;             // this thread's 8 x 8 piece
     const T *x = static_cast<const T *>(Q.x);
 
-    float v[8][8];
+    Piece<T> v;
+    if (VEC && row + 8 <= Q.rows && col + 8 <= Q.cols) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const T *p = x + (long long)(row + i) * Q.ldx + col;
-        if (row + i < Q.rows && col + 8 <= Q.cols && VEC) {
-            load8(p, v[i]);
-        } else {
+        for (int i = 0; i < 8; ++i) v.load(i, x + (long long)(row + i) * Q.ldx + col);
+    } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = row + i < Q.rows && col + j < Q.cols ? to_f32(p[j]) : 0.0f;
-        }
-    }
-    // maxima of magnitudes (fmaxf drops a NaN: it does not enter a group's scale)
-    float rmax[8], cmax[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        rmax[i] = 0.0f;
-        if (i == 0)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) cmax[j] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            rmax[i] = fmaxf(rmax[i], fabsf(v[i][j]));
-            if (BOTH && !BLOCKS) cmax[j] = fmaxf(cmax[j], fabsf(v[i][j]));
+        for (int i = 0; i < 8; ++i) {
+            const T *p = x + (long long)(row + i) * Q.ldx + col;
+            if (VEC && row + i < Q.rows && col + 8 <= Q.cols) v.load(i, p);
+            else v.load_some(i, p, row + i < Q.rows ? Q.cols - col : 0);
         }
     }
     float rrec[8], crec[8];
     if (BLOCKS) {
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, rmax[i]);
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, v.row_max(i));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         if (lane == 0) part[warp][0] = m;
@@ -106,43 +192,50 @@ quantize_fp8_kernel(const QuantFp8 Q)
             if (BOTH) Q.scales_t[(long long)ti * Q.tiles_j + tj] = s;
         }
     } else {
+        if (BOTH) v.column_max(&part[warp][tx * 8], lane);
+        // Row maxima over sixteen lanes: each exchange halves the number of rows a lane is left with (8 shuffles instead of
+        // 32), so that a lane ends with one row, whose scale it computes once and hands back.
+        float m[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 8; ++i) m[i] = v.row_max(i);
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) rmax[i] = fmaxf(rmax[i], __shfl_xor_sync(0xffffffffu, rmax[i], o));
-            float s;
-            scale_of(rmax[i], s, rrec[i]);
-            if (tx == i && row + i < Q.rows) Q.scales[(long long)tj * Q.rows + row + i] = s;
+        for (int i = 0; i < 4; ++i) {
+            const float keep = (tx & 8) ? m[i + 4] : m[i], send = (tx & 8) ? m[i] : m[i + 4];
+            m[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, send, 8));
         }
-        if (BOTH) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) cmax[j] = fmaxf(cmax[j], __shfl_xor_sync(0xffffffffu, cmax[j], 16));
-            if (lane < 16) {
-                *reinterpret_cast<float4 *>(&part[warp][tx * 8]) = make_float4(cmax[0], cmax[1], cmax[2], cmax[3]);
-                *reinterpret_cast<float4 *>(&part[warp][tx * 8 + 4]) = make_float4(cmax[4], cmax[5], cmax[6], cmax[7]);
-            }
+        for (int i = 0; i < 2; ++i) {
+            const float keep = (tx & 4) ? m[i + 2] : m[i], send = (tx & 4) ? m[i] : m[i + 2];
+            m[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, send, 4));
+        }
+        const float keep = (tx & 2) ? m[1] : m[0], send = (tx & 2) ? m[0] : m[1];
+        m[0] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, send, 2));
+        m[0] = fmaxf(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
+        float s, r;
+        scale_of(fmaxf(m[0], 0.0f), s, r);
+        const int mine = tx >> 1;                                // the row this lane was left with
+        if ((tx & 1) == 0 && row + mine < Q.rows) Q.scales[(long long)tj * Q.rows + row + mine] = s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rrec[i] = __shfl_sync(0xffffffffu, r, (lane & 16) | (i << 1));
+        if (BOTH) {
             __syncthreads();
             if (threadIdx.x < 128) {        // one column each; the reciprocal goes back through part[0]
-                float m = part[0][threadIdx.x];
+                float mc = part[0][threadIdx.x];
 #pragma unroll
-                for (int k = 1; k < 8; ++k) m = fmaxf(m, part[k][threadIdx.x]);
-                float s, r;
-                scale_of(m, s, r);
+                for (int k = 1; k < 8; ++k) mc = fmaxf(mc, part[k][threadIdx.x]);
+                scale_of(mc, s, r);
                 part[0][threadIdx.x] = r;
                 if (c0 + (int)threadIdx.x < Q.cols) Q.scales_t[(long long)ti * Q.cols + c0 + threadIdx.x] = s;
             }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < 8; ++j) crec[j] = part[0][tx * 8 + j];
         }
     }
-    {
+    if (col < Q.cols) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (row + i >= Q.rows || col >= Q.cols) continue;
+            if (row + i >= Q.rows) break;
             uint32_t h[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = code2(__fmul_rn(v[i][2 * j], rrec[i]), __fmul_rn(v[i][2 * j + 1], rrec[i]));
+            for (int j = 0; j < 4; ++j) h[j] = code2(__fmul_rn(v.value(i, 2 * j), rrec[i]), __fmul_rn(v.value(i, 2 * j + 1), rrec[i]));
             unsigned char *p = Q.codes + (long long)(row + i) * Q.ldc + col;
             if (col + 8 <= Q.cols) *reinterpret_cast<uint2 *>(p) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
             else
@@ -152,11 +245,17 @@ quantize_fp8_kernel(const QuantFp8 Q)
         }
     }
     if (BOTH) {
+        if (!BLOCKS) {
+            __syncthreads();
+            const float4 a = *reinterpret_cast<const float4 *>(&part[0][tx * 8]), b = *reinterpret_cast<const float4 *>(&part[0][tx * 8 + 4]);
+            crec[0] = a.x; crec[1] = a.y; crec[2] = a.z; crec[3] = a.w;
+            crec[4] = b.x; crec[5] = b.y; crec[6] = b.z; crec[7] = b.w;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             uint32_t h[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = code2(__fmul_rn(v[2 * i][j], crec[j]), __fmul_rn(v[2 * i + 1][j], crec[j]));
+            for (int i = 0; i < 4; ++i) h[i] = code2(__fmul_rn(v.value(2 * i, j), crec[j]), __fmul_rn(v.value(2 * i + 1, j), crec[j]));
             *reinterpret_cast<uint2 *>(&tile_t[(tx * 8 + j) * 128 + ((ty ^ tx) << 3)]) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
         }
         __syncthreads();

@@ -42,23 +42,39 @@ constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr size_t kStatusBytes = 256;
 
+constexpr int kMaxSlots = 80;                          // CTA pairs of a launch (74 on a B200)
+
+// One product of a launch: output I x J, reduced over R, cut into `splits` parts of the reduced dimension.
+struct LossJob {
+    int mode;
+    int I, J, R;
+    int tiles_i, tiles_j, splits;
+    // Backward: its units (tile, split) on the launch's slots: slot s takes units i * slots + s for i < rounds, then extra[s] .. extra[s + 1] - 1.
+    int rounds;
+    int extra[kMaxSlots + 1];
+};
+struct LossMaps {
+    CUtensorMap a[3], b[3], o[3];
+};
+
 struct LossParams {
-    int I, J, R;                    // output rows, output columns, reduced entries
-    int tiles_i, tiles_j, slots;
+    LossJob job[3];
+    int jobs, slots;
     const long long *labels;        // STATS, DLOGIT
-    int v0;                         // word of column 0 (DLOGIT: first word of the piece)
+    int V;                          // words of the vocabulary
+    int v0;                         // DLOGIT: first word of the piece
     float2 *part;                   // STATS: (maximum, sum) per row and half tile
     int parts;                      // ... entries per row
-    int V;                          // DLOGIT: words of the whole vocabulary
     float *target;                  // STATS: the label's logit
     const float *lse, *dloss;       // DLOGIT
     const float *scale;             // backward: {S, 1/S}, what dl is stored with
-    int first, last;                // DH: first / last piece
-    void *out;                      // DW, last DH: output, row pitch ldo, stored directly unless out_tma
-    long long ldo;
-    int out_tma;
-    float *acc;                     // DH: binary32 sums, row pitch acc_ld
+    int first, last;                // DH: first / last piece (last: the output itself is written, unless the job is split)
+    float *acc;                     // DH: binary32 sums of the pieces so far, row pitch acc_ld, acc_rows rows per split
     long long acc_ld;
+    int acc_rows;
+    void *out_w, *out_h;            // DW, DH: outputs, row pitches; stored by the threads unless out_tma
+    long long ldw, ldh;
+    int out_tma;
     int *status;
 };
 
@@ -77,17 +93,62 @@ __device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti
     ti = first + in - tj * rows;
 }
 
-template <bool PAIR, int MODE, typename T>
+// The units of a slot, in order.
+struct LossWalk {
+    int j, i;
+};
+struct LossUnit {
+    int j, ti, tj, split, rb0, rb1;     // j < 0: no more
+};
+template <bool GRAD>
+__device__ __forceinline__ LossUnit next_unit(LossWalk &w, const LossParams &P, int slot)
+{
+    LossUnit u;
+    u.j = -1;
+    if constexpr (!GRAD) {                                      // one job of whole tiles, taken in turn
+        const LossJob &J = P.job[0];
+        const int n = w.i * P.slots + slot;
+        if (n >= J.tiles_i * J.tiles_j) return u;
+        ++w.i;
+        u.j = 0;
+        u.split = 0;
+        tile_at(n, J.tiles_i, J.tiles_j, u.ti, u.tj);
+        u.rb0 = 0;
+        u.rb1 = (J.R + kBK - 1) / kBK;
+        return u;
+    } else {
+        while (w.j < P.jobs) {
+            const LossJob &J = P.job[w.j];
+            int n = w.i * P.slots + slot;
+            if (w.i >= J.rounds) n = J.extra[slot] + (w.i - J.rounds);
+            if (w.i < J.rounds || n < J.extra[slot + 1]) {
+                ++w.i;
+                u.j = w.j;
+                const int t = J.splits == 1 ? n : n / J.splits;
+                u.split = n - t * J.splits;
+                tile_at(t, J.tiles_i, J.tiles_j, u.ti, u.tj);
+                const int rblocks = (J.R + kBK - 1) / kBK;
+                u.rb0 = J.splits == 1 ? 0 : (int)((long long)rblocks * u.split / J.splits);
+                u.rb1 = J.splits == 1 ? rblocks : (int)((long long)rblocks * (u.split + 1) / J.splits);
+                return u;
+            }
+            ++w.j;
+            w.i = 0;
+        }
+        return u;
+    }
+}
+
+// GRAD: a launch of the backward pass (jobs DLOGIT, DW and DH in any mixture); otherwise STATS alone.
+template <bool PAIR, bool GRAD, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
-loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                 const __grid_constant__ CUtensorMap map_o, const __grid_constant__ CUtensorMap map_f, const LossParams P)
+loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ LossParams P)
 {
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 4];
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s;
 
-    constexpr bool kAMn = MODE == DW, kBMn = MODE == DW || MODE == DH;
     constexpr int kBRows = PAIR ? 128 : 256;           // columns of the tile that this CTA stages
     constexpr uint32_t kBBytes = (uint32_t)kBRows * 128u;
     constexpr uint32_t kStageBytes = (uint32_t)kBlockBytes + kBBytes;
@@ -98,7 +159,6 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     volatile int *abort_flag = &abort_s;
     const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
     const int slot = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
-    const int units = P.tiles_i * P.tiles_j, rblocks = (P.R + kBK - 1) / kBK;
 
     const uint32_t bar0 = smem_u32(&bars[0]);
     constexpr uint32_t kEmptyOff = 8u * kStagesMax;
@@ -131,12 +191,16 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (PAIR) tma_load_2d_pair(dst, map, c0, c1, fb);
                 else tma_load_2d(dst, map, c0, c1, fb);
             };
-            for (int u = slot; u < units && !failed; u += P.slots) {
-                int ti, tj;
-                tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
-                const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
-                const int brow = tj * 256 + (PAIR ? (int)rank * 128 : 0);
-                for (int rb = 0; rb < rblocks; ++rb) {
+            LossWalk walk{0, 0};
+            while (!failed) {
+                const LossUnit u = next_unit<GRAD>(walk, P, slot);
+                if (u.j < 0) break;
+                const int mode = GRAD ? P.job[u.j].mode : STATS;
+                const bool a_mn = mode == DW, b_mn = mode == DW || mode == DH;
+                const CUtensorMap *map_a = &maps.a[u.j], *map_b = &maps.b[u.j];
+                const int arow = u.ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
+                const int brow = u.tj * 256 + (PAIR ? (int)rank * 128 : 0);
+                for (int rb = u.rb0; rb < u.rb1; ++rb) {
                     const uint32_t fb = bar0 + 8u * st;
                     if (!mbar_try_wait_now(fb + kEmptyOff, par) && !mbar_wait(fb + kEmptyOff, par, abort_flag, kWaitNs)) {
                         failed = true;
@@ -147,14 +211,14 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     if (!PAIR || rank == 0) mbar_expect_tx(fb, (PAIR ? 2u : 1u) * kStageBytes);
                     // K-major: one box of 64 reduced entries x the block's rows.  MN-major: boxes of 64 rows x 64
                     // reduced entries, the stored matrix's rows being the reduced dimension.
-                    if (kAMn) {
-                        load(sa, &map_a, arow, r, fb);
-                        load(sa + 8192u, &map_a, arow + 64, r, fb);
-                    } else load(sa, &map_a, r, arow, fb);
-                    if (kBMn) {
+                    if (a_mn) {
+                        load(sa, map_a, arow, r, fb);
+                        load(sa + 8192u, map_a, arow + 64, r, fb);
+                    } else load(sa, map_a, r, arow, fb);
+                    if (b_mn) {
 #pragma unroll
-                        for (int b = 0; b < kBRows / 64; ++b) load(sb + (uint32_t)b * 8192u, &map_b, brow + b * 64, r, fb);
-                    } else load(sb, &map_b, r, brow, fb);
+                        for (int b = 0; b < kBRows / 64; ++b) load(sb + (uint32_t)b * 8192u, map_b, brow + b * 64, r, fb);
+                    } else load(sb, map_b, r, brow, fb);
                     if (++st == (uint32_t)kStages) {
                         st = 0u;
                         par ^= 1u;
@@ -167,22 +231,27 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         if (lane == 0 && (!PAIR || rank == 0)) {
             // K-major: 128-byte rows, groups of eight 1024 bytes apart, 32 bytes per MMA.  MN-major: one reduced entry per
             // 128-byte line, eight lines 1024 bytes apart, 64-row blocks 8192 bytes apart, 16 lines per MMA.
-            const uint64_t a_d = kAMn ? make_desc(smem_base, 8192, 1024) : make_desc(smem_base, 16, 1024);
-            const uint64_t b_d = kBMn ? make_desc(smem_base + kBlockBytes, 8192, 1024) : make_desc(smem_base + kBlockBytes, 16, 1024);
-            const uint32_t a_hi = (uint32_t)(a_d >> 32), b_hi = (uint32_t)(b_d >> 32), a_lo0 = (uint32_t)a_d, b_lo0 = (uint32_t)b_d;
-            constexpr uint32_t a_step = kAMn ? 2048u >> 4 : 2u, b_step = kBMn ? 2048u >> 4 : 2u;
-            constexpr uint32_t kFmt = sizeof(T) == 2 && __is_same(T, __nv_bfloat16) ? 1u : 0u;
-            const uint32_t idesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((kAMn ? 1u : 0u) << 15) | ((kBMn ? 1u : 0u) << 16) |
-                                   ((256u >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
+            const uint64_t k_d = make_desc(smem_base, 16, 1024), mn_d = make_desc(smem_base, 8192, 1024);
+            const uint32_t d_hi = (uint32_t)(k_d >> 32), k_lo = (uint32_t)k_d, mn_lo = (uint32_t)mn_d;      // (the upper words agree)
+            constexpr uint32_t kFmt = __is_same(T, __nv_bfloat16) ? 1u : 0u;
+            const uint32_t idesc0 = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((256u >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
             uint32_t st = 0u, par = 0u, buf = 0u, tpar = 1u;
-            for (int u = slot; u < units && !failed; u += P.slots) {
+            LossWalk walk{0, 0};
+            while (!failed) {
+                const LossUnit u = next_unit<GRAD>(walk, P, slot);
+                if (u.j < 0) break;
+                const int mode = GRAD ? P.job[u.j].mode : STATS;
+                const bool a_mn = mode == DW, b_mn = mode == DW || mode == DH;
+                const uint32_t a_lo0 = a_mn ? mn_lo : k_lo, b_lo0 = (b_mn ? mn_lo : k_lo) + (uint32_t)(kBlockBytes >> 4);
+                const uint32_t a_step = a_mn ? 2048u >> 4 : 2u, b_step = b_mn ? 2048u >> 4 : 2u;
+                const uint32_t idesc = idesc0 | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16);
                 if (!mbar_try_wait_now(tempty0 + 8u * buf, tpar) && !mbar_wait(tempty0 + 8u * buf, tpar, abort_flag, kWaitNs)) {
                     failed = true;
                     break;
                 }
                 tc_fence_after();
                 uint32_t accumulate = 0u;
-                for (int rb = 0; rb < rblocks; ++rb) {
+                for (int rb = u.rb0; rb < u.rb1; ++rb) {
                     const uint32_t fb = bar0 + 8u * st;
                     if (!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs)) {
                         failed = true;
@@ -190,7 +259,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                     tc_fence_after();
                     const uint32_t off = st * (kStageBytes >> 4);
-                    tc_mma4<PAIR, KIND_F16>(tmem_base + buf * 256u, a_lo0 + off, a_hi, a_step, b_lo0 + off, b_hi, b_step, idesc, accumulate);
+                    tc_mma4<PAIR, KIND_F16>(tmem_base + buf * 256u, a_lo0 + off, d_hi, a_step, b_lo0 + off, d_hi, b_step, idesc, accumulate);
                     accumulate = 1u;
                     if (PAIR) tc_commit_pair(fb + kEmptyOff);
                     else tc_commit(fb + kEmptyOff);
@@ -211,7 +280,7 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         // ------------------------------------------------------------ epilogue warps: 32 rows x 128 columns each
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t wbuf = smem_base + (uint32_t)kStagesMax * 2u * kBlockBytes + (uint32_t)((warp - 2) * kOutWarpBytes);
-        const float unscale = MODE == DW || MODE == DH ? P.scale[1] : 1.0f;
+        const float unscale = GRAD ? P.scale[1] : 1.0f;
         uint32_t buf = 0u, tpar = 0u;
         // 128 bytes of each of the warp's rows -> staging block -> TMA box at (col, row0)
         auto send = [&](const uint32_t (&w)[32], const CUtensorMap *map, bool add, int col, int row0) {
@@ -231,21 +300,24 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 bulk_commit();
             }
         };
-        for (int u = slot; u < units && !failed; u += P.slots) {
-            int ti, tj;
-            tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
-            const int row0 = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
-            const int col0 = tj * 256 + half * 128;
+        LossWalk walk{0, 0};
+        while (!failed) {
+            const LossUnit u = next_unit<GRAD>(walk, P, slot);
+            if (u.j < 0) break;
+            const int mode = GRAD ? P.job[u.j].mode : STATS;
+            const int I = P.job[u.j].I, J = P.job[u.j].J;
+            const CUtensorMap *map_o = &maps.o[u.j];
+            const int row0 = u.ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
+            const int col0 = u.tj * 256 + half * 128;
             const int row = row0 + lane;
             // what the epilogue needs of its row, fetched while the products run
             int label = -1;                              // column of the row's label in this tile's matrix, or outside it
             float lse2 = 0.0f, g = 0.0f;
-            if ((MODE == STATS || MODE == DLOGIT) && row < P.I) {
+            if ((!GRAD || mode == DLOGIT) && row < I) {
                 const long long y = P.labels[row];
-                const long long words = MODE == STATS ? (long long)P.J : 0x7fffffffll;
-                const long long c = y - P.v0;
-                label = y >= 0 && c >= 0 && c < words ? (int)c : -1;
-                if (MODE == DLOGIT) {
+                const long long c = y - (GRAD ? P.v0 : 0);
+                label = c >= 0 && y < P.V ? (int)c : -1;
+                if (GRAD) {
                     lse2 = P.lse[row] * kLog2e;
                     // (a label outside the vocabulary: no gradient)
                     g = y >= 0 && y < P.V ? P.dloss[row] * P.scale[0] : 0.0f;
@@ -258,22 +330,22 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * 256u + (uint32_t)(half * 128);
-            const bool live = row0 < P.I && col0 < P.J;          // uniform over the warp
+            const bool live = row0 < I && col0 < J;          // uniform over the warp
             if (live) {
-                if (MODE == STATS) {
+                if (!GRAD) {
                     float m = -INFINITY, s = 0.0f, tgt = 0.0f;
                     bool hit = false;
 #pragma unroll 1
                     for (int ch = 0; ch < 4; ++ch) {
                         const int c0 = col0 + ch * 32;
-                        if (c0 >= P.J) break;
+                        if (c0 >= J) break;
                         uint32_t v[32];
                         tc_ld32(taddr + (uint32_t)(ch * 32), v);
                         tc_wait_ld_pin(v);
-                        if (c0 + 32 > P.J) {
+                        if (c0 + 32 > J) {
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
-                                if (c0 + c >= P.J) v[c] = 0xff800000u;       // a column that does not exist: -infinity
+                                if (c0 + c >= J) v[c] = 0xff800000u;       // a column that does not exist: -infinity
                         }
                         if (__any_sync(0xffffffffu, (unsigned)(label - c0) < 32u)) {
 #pragma unroll
@@ -299,15 +371,15 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         s = s * (m == -INFINITY ? 0.0f : exp2_fast(fmaf(m, kLog2e, -base))) + ((s0 + s1) + (s2 + s3));
                         m = mn;
                     }
-                    if (row < P.I) {
-                        P.part[(long long)row * P.parts + 2 * tj + half] = make_float2(m, s);
+                    if (row < I) {
+                        P.part[(long long)row * P.parts + 2 * u.tj + half] = make_float2(m, s);
                         if (hit) P.target[row] = tgt;
                     }
-                } else if (MODE == DLOGIT) {
+                } else if (mode == DLOGIT) {
 #pragma unroll 1
                     for (int ch = 0; ch < 2; ++ch) {
                         const int c0 = col0 + ch * 64;
-                        if (c0 >= P.J) break;
+                        if (c0 >= J) break;
                         uint32_t w[32];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
@@ -329,20 +401,20 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                                 w[16 * h + c] = pack2<T>(d0, d1);
                             }
                         }
-                        send(w, &map_o, false, c0, row0);
+                        send(w, map_o, false, c0, row0);
                     }
-                } else if (MODE == DW || (MODE == DH && P.last)) {
+                } else if (mode == DW || (P.last && P.job[u.j].splits == 1)) {
 #pragma unroll 1
                     for (int ch = 0; ch < 2; ++ch) {
                         const int c0 = col0 + ch * 64;
-                        if (c0 >= P.J) break;
+                        if (c0 >= J) break;
                         uint32_t w[32];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t v[32];
                             tc_ld32(taddr + (uint32_t)(ch * 64 + h * 32), v);
                             tc_wait_ld_pin(v);
-                            if (MODE == DH && !P.first && row < P.I) {       // what the earlier pieces have summed
+                            if (mode == DH && !P.first && row < I) {       // what the earlier pieces have summed
                                 const float4 *q = reinterpret_cast<const float4 *>(P.acc + (long long)row * P.acc_ld + c0 + 32 * h);
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) {
@@ -357,16 +429,16 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             for (int c = 0; c < 16; ++c)
                                 w[16 * h + c] = pack2<T>(__uint_as_float(v[2 * c]) * unscale, __uint_as_float(v[2 * c + 1]) * unscale);
                         }
-                        if (P.out_tma) send(w, &map_o, false, c0, row0);
-                        else if (row < P.I) {
-                            T *o = static_cast<T *>(P.out) + (long long)row * P.ldo + c0;
+                        if (P.out_tma) send(w, map_o, false, c0, row0);
+                        else if (row < I) {
+                            T *o = static_cast<T *>(mode == DW ? P.out_w : P.out_h) + (long long)row * (mode == DW ? P.ldw : P.ldh) + c0;
 #pragma unroll
                             for (int c = 0; c < 8; ++c) {
-                                if (c0 + 8 * c + 8 <= P.J) *reinterpret_cast<uint4 *>(o + 8 * c) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+                                if (c0 + 8 * c + 8 <= J) *reinterpret_cast<uint4 *>(o + 8 * c) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
                                 else
 #pragma unroll
                                     for (int j = 0; j < 8; ++j)
-                                        if (c0 + 8 * c + j < P.J)
+                                        if (c0 + 8 * c + j < J)
                                             reinterpret_cast<unsigned short *>(o)[8 * c + j] = (unsigned short)(w[4 * c + (j >> 1)] >> (16 * (j & 1)));
                             }
                         }
@@ -375,11 +447,15 @@ loss_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 #pragma unroll 1
                     for (int ch = 0; ch < 4; ++ch) {
                         const int c0 = col0 + ch * 32;
-                        if (c0 >= P.J) break;
+                        if (c0 >= J) break;
                         uint32_t v[32];
                         tc_ld32(taddr + (uint32_t)(ch * 32), v);
                         tc_wait_ld_pin(v);
-                        send(v, &map_f, !P.first, c0, row0);
+                        if (u.rb0 == u.rb1) {            // a last piece too short for all splits: nothing was multiplied
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) v[c] = 0u;
+                        }
+                        send(v, map_o, !P.first, c0, u.split * P.acc_rows + row0);
                     }
                 }
             }
@@ -471,32 +547,65 @@ loss_scale_kernel(const float *__restrict__ dloss, const long long *__restrict__
     }
 }
 
+// dH from the binary32 sums of the splits, added in their order
 template <typename T>
-const void *variant(int mode, bool pair)
+__global__ void __launch_bounds__(256)
+loss_sum_kernel(const float *__restrict__ acc, long long acc_ld, long long split_elems, int splits, int rows, int cols,
+                const float *__restrict__ scale, T *__restrict__ out, long long ldo)
 {
-    switch (mode) {
-    case STATS: return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, STATS, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, STATS, T>);
-    case DLOGIT: return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, DLOGIT, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, DLOGIT, T>);
-    case DW: return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, DW, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, DW, T>);
-    default: return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, DH, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, DH, T>);
+    const float unscale = scale[1];
+    const int per_row = (cols + 7) / 8;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)rows * per_row; i += (long long)gridDim.x * 256) {
+        const long long r = i / per_row;
+        const int c = (int)(i - r * per_row) * 8;
+        const float *p = acc + r * acc_ld + c;
+        float v[8];
+        load8(p, v);
+        for (int s = 1; s < splits; ++s) {
+            float w[8];
+            load8(p + s * split_elems, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += w[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= unscale;
+        T *o = out + r * ldo + c;
+        if (c + 8 <= cols) store8(o, v);
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < cols) o[k] = from_f32<T>(v[k]);
     }
 }
-const void *variant(int mode, bool pair, int type) { return type == CDL_BF16 ? variant<__nv_bfloat16>(mode, pair) : variant<__half>(mode, pair); }
+
+template <typename T>
+const void *variant(bool pair, bool grad)
+{
+    if (grad) return reinterpret_cast<const void *>(&loss_gemm_kernel<true, true, T>);
+    return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, false, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, false, T>);
+}
+const void *variant(bool pair, bool grad, int type) { return type == CDL_BF16 ? variant<__nv_bfloat16>(pair, grad) : variant<__half>(pair, grad); }
 
 inline size_t up256(size_t n) { return (n + 255u) & ~(size_t)255u; }
+inline int tiles256(long long n) { return (int)((n + 255) / 256); }
 
 // Layout of the workspace.  The forward part (partial statistics) and the backward part share the space after the status
 // block and the scale.
 struct LossPlan {
     int parts;              // partial statistics per row
     int pieces, Vp;         // vocabulary pieces of the backward pass and their width (a multiple of 256)
+    int splits;             // parts of the vocabulary piece that dH's product is cut into
     size_t off_target;      // forward
-    size_t off_acc;         // backward: binary32 sums of dH
+    size_t dl_bytes;        // backward: dl of one piece (two of them when there are several pieces)
+    size_t off_acc;         // backward: binary32 sums of dH, [splits][acc_rows][acc_ld]
     long long acc_ld;
+    int acc_rows;
     size_t fwd_bytes, bwd_bytes;
 };
 constexpr size_t kOffScale = kStatusBytes, kOffData = kStatusBytes + 256;
-constexpr long long kPieceBytes = 64ll << 20;          // dl of one piece: half of L2
+constexpr long long kPieceBytes = 64ll << 20;          // dl of one piece
+constexpr long long kAccBytes = 64ll << 20;            // most that the splits of dH's product may add up to
+constexpr int kPlanSlots = 74;                         // B200: planned for this count so that workspace sizes are fixed
 
 LossPlan make_plan(int T, int V, int D)
 {
@@ -504,44 +613,107 @@ LossPlan make_plan(int T, int V, int D)
     p.parts = (int)(((long long)V + 127) / 128);
     p.off_target = kOffData + up256((size_t)T * (size_t)p.parts * sizeof(float2));
     p.fwd_bytes = p.off_target + up256((size_t)T * sizeof(float));
-    const long long words = ((long long)V + 255) / 256;                 // in units of 256
+    const long long words = tiles256(V);                // in units of 256
     long long most = kPieceBytes / (512ll * (T > 0 ? T : 1));
     if (most < 8) most = 8;
     p.pieces = (int)((words + most - 1) / most);
     p.Vp = (int)((words + p.pieces - 1) / p.pieces) * 256;
     p.pieces = (int)((V + (long long)p.Vp - 1) / p.Vp);
-    p.acc_ld = ((long long)D + 255) / 256 * 256;
-    p.off_acc = kOffData + up256((size_t)T * (size_t)p.Vp * 2);
-    p.bwd_bytes = p.off_acc + (p.pieces > 1 ? up256((size_t)T * (size_t)p.acc_ld * sizeof(float)) : 0);
+    p.acc_ld = (long long)tiles256(D) * 256;
+    p.acc_rows = tiles256(T) * 256;
+    // dH has few tiles, each as long as the piece: cut so that a part is at most a third of a slot's share of the launch
+    const long long ti = tiles256(T), td = tiles256(D), wp = p.Vp / 256;
+    const long long len_h = p.Vp / kBK, len_w = (T + kBK - 1) / kBK;
+    const long long share = (ti * td * len_h + wp * td * len_w) / kPlanSlots + 1;
+    long long s = (3 * len_h + share - 1) / share;
+    if (s > len_h / 8) s = len_h / 8;
+    if (s > kAccBytes / (4 * p.acc_rows * p.acc_ld + 1)) s = kAccBytes / (4 * p.acc_rows * p.acc_ld + 1);
+    if (s > 16) s = 16;
+    p.splits = s > 1 ? (int)s : 1;
+    p.dl_bytes = up256((size_t)T * (size_t)p.Vp * 2);
+    p.off_acc = kOffData + p.dl_bytes * (p.pieces > 1 ? 2 : 1);
+    p.bwd_bytes = p.off_acc + (p.pieces > 1 || p.splits > 1 ? up256((size_t)p.splits * (size_t)p.acc_rows * (size_t)p.acc_ld * sizeof(float)) : 0);
     return p;
 }
 
-// One product: output I x J, reduced over R.  a_mn / b_mn operands are stored [R][I] / [R][J].
-int launch_product(int mode, int type, const void *A, long long lda, const void *B, long long ldb, const void *out, long long ldo,
-                   const void *facc, long long ldf, LossParams &P, cudaStream_t stream)
+// Spreads the units of the launch's jobs over the slots: longest units first, each job's counts chosen so that the slots'
+// loads (in pipeline stages, and two for a unit's epilogue) fill to one level.
+void spread_units(LossParams &P)
+{
+    int order[3] = {0, 1, 2};
+    long long len[3], load[kMaxSlots];
+    for (int j = 0; j < P.jobs; ++j) len[j] = ((P.job[j].R + kBK - 1) / kBK + P.job[j].splits - 1) / P.job[j].splits + 2;
+    for (int a = 0; a < P.jobs; ++a)                     // longest first
+        for (int b = a + 1; b < P.jobs; ++b)
+            if (len[order[b]] > len[order[a]]) {
+                const int t = order[a];
+                order[a] = order[b];
+                order[b] = t;
+            }
+    for (int s = 0; s < P.slots; ++s) load[s] = 0;
+    for (int a = 0; a < P.jobs; ++a) {
+        LossJob &J = P.job[order[a]];
+        const long long n = (long long)J.tiles_i * J.tiles_j * J.splits, L = len[order[a]];
+        long long lo = 0, hi = 0;
+        for (int s = 0; s < P.slots; ++s) hi = load[s] > hi ? load[s] : hi;
+        hi += (n / P.slots + 2) * L;
+        auto count = [&](long long level, int s) { return level > load[s] ? (level - load[s]) / L : 0; };
+        while (lo < hi) {                               // the lowest level that holds all n units
+            const long long mid = (lo + hi) / 2;
+            long long have = 0;
+            for (int s = 0; s < P.slots; ++s) have += count(mid, s);
+            if (have >= n) hi = mid;
+            else lo = mid + 1;
+        }
+        long long c[kMaxSlots], over = -n, least;
+        for (int s = 0; s < P.slots; ++s) over += c[s] = count(lo, s);
+        for (int s = 0; s < P.slots && over > 0; ++s)
+            if (c[s] > 0 && load[s] + c[s] * L == lo) {  // (those that reach the level exactly came in with it)
+                --c[s];
+                --over;
+            }
+        least = c[0];
+        for (int s = 1; s < P.slots; ++s) least = c[s] < least ? c[s] : least;
+        J.rounds = (int)least;
+        J.extra[0] = (int)least * P.slots;
+        for (int s = 0; s < P.slots; ++s) {
+            J.extra[s + 1] = J.extra[s] + (int)(c[s] - least);
+            load[s] += c[s] * L;
+        }
+    }
+}
+
+// Adds a product to a launch.  Operands whose rows are the reduced dimension (MN-major) are stored [R][I] / [R][J].
+bool add_job(LossParams &P, LossMaps &maps, int type, bool pair, int mode, int I, int J, int R, int splits, const void *A, long long lda,
+             const void *B, long long ldb)
+{
+    LossJob &job = P.job[P.jobs];
+    job.mode = mode;
+    job.I = I;
+    job.J = J;
+    job.R = R;
+    job.tiles_i = pair ? tiles256(I) : (int)(((long long)I + 127) / 128);
+    job.tiles_j = tiles256(J);
+    job.splits = splits;
+    const CUtensorMapDataType dt = type == CDL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const bool a_mn = mode == DW, b_mn = mode == DW || mode == DH;
+    const int k = P.jobs++;
+    return (a_mn ? encode_map_2d(&maps.a[k], dt, 2, A, (uint64_t)I, (uint64_t)R, (uint64_t)lda * 2, 64)
+                 : encode_map_2d(&maps.a[k], dt, 2, A, (uint64_t)R, (uint64_t)I, (uint64_t)lda * 2, 128)) &&
+           (b_mn ? encode_map_2d(&maps.b[k], dt, 2, B, (uint64_t)J, (uint64_t)R, (uint64_t)ldb * 2, 64)
+                 : encode_map_2d(&maps.b[k], dt, 2, B, (uint64_t)R, (uint64_t)J, (uint64_t)ldb * 2, pair ? 128 : 256));
+}
+bool set_output(LossMaps &maps, int k, int type, const void *out, uint64_t cols, uint64_t rows, long long ld)
+{
+    const CUtensorMapDataType dt = type == CDL_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                                   : (type == CDL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+    return encode_map_2d(&maps.o[k], dt, type_bytes(type), out, cols, rows, (uint64_t)ld * (uint64_t)type_bytes(type), 32);
+}
+
+int launch_jobs(bool pair, bool grad, int type, LossMaps &maps, LossParams &P, cudaStream_t stream)
 {
     const int sms = sm_count();
     if (sms <= 0) return CDL_ERR_LAUNCH;
-    const bool pair = P.I > 128;
-    const bool a_mn = mode == DW, b_mn = mode == DW || mode == DH;
-    const CUtensorMapDataType dt = type == CDL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    CUtensorMap map_a, map_b, map_o, map_f;
-    bool ok = a_mn ? encode_map_2d(&map_a, dt, 2, A, (uint64_t)P.I, (uint64_t)P.R, (uint64_t)lda * 2, 64)
-                   : encode_map_2d(&map_a, dt, 2, A, (uint64_t)P.R, (uint64_t)P.I, (uint64_t)lda * 2, 128);
-    ok = ok && (b_mn ? encode_map_2d(&map_b, dt, 2, B, (uint64_t)P.J, (uint64_t)P.R, (uint64_t)ldb * 2, 64)
-                     : encode_map_2d(&map_b, dt, 2, B, (uint64_t)P.R, (uint64_t)P.J, (uint64_t)ldb * 2, pair ? 128 : 256));
-    map_o = map_a;
-    map_f = map_a;
-    if (out != nullptr) ok = ok && encode_map_2d(&map_o, dt, 2, out, (uint64_t)P.J, (uint64_t)P.I, (uint64_t)ldo * 2, 32);
-    if (facc != nullptr) ok = ok && encode_map_2d(&map_f, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, facc, (uint64_t)P.J, (uint64_t)P.I, (uint64_t)ldf * 4, 32);
-    if (!ok) return CDL_ERR_LAUNCH;
-    // (a TMA store fills the last 16-byte unit of a row with zeros beyond the output's columns: rows of a caller's matrix
-    // that do not end on one are stored by the threads)
-    P.out = const_cast<void *>(out);
-    P.ldo = ldo;
-    P.out_tma = P.J % 8 == 0;
-    P.tiles_i = pair ? (P.I + 255) / 256 : (P.I + 127) / 128;
-    P.tiles_j = (P.J + 255) / 256;
     static bool attr_set[64];
     static int pair_slots[64];
     int dev = 0;
@@ -556,31 +728,33 @@ int launch_product(int mode, int type, const void *A, long long lda, const void 
     cfg.dynamicSmemBytes = kSmemBytes;
     cfg.attrs = at;
     if (!attr_set[dev]) {
-        for (int m = 0; m < 4; ++m)
-            for (int v = 0; v < 4; ++v)
-                if (cudaFuncSetAttribute(variant(m, (v & 1) != 0, (v & 2) != 0 ? CDL_BF16 : CDL_F16), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) {
-                    (void)cudaGetLastError();
-                    return CDL_ERR_LAUNCH;
-                }
+        for (int v = 0; v < 8; ++v)
+            if (cudaFuncSetAttribute(variant((v & 1) != 0, (v & 2) != 0, (v & 4) != 0 ? CDL_BF16 : CDL_F16), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) {
+                (void)cudaGetLastError();
+                return CDL_ERR_LAUNCH;
+            }
         cfg.gridDim = dim3(2u * (unsigned)(sms / 2));
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, variant(STATS, true, CDL_BF16), &cfg) != cudaSuccess || n < 1) {
+        if (cudaOccupancyMaxActiveClusters(&n, variant(true, true, CDL_BF16), &cfg) != cudaSuccess || n < 1) {
             (void)cudaGetLastError();
             n = sms / 2;
         }
-        pair_slots[dev] = n < sms / 2 ? n : sms / 2;
+        n = n < sms / 2 ? n : sms / 2;
+        pair_slots[dev] = n < kMaxSlots ? n : kMaxSlots;
         attr_set[dev] = true;
     }
-    const long long units = (long long)P.tiles_i * P.tiles_j;
-    if (units > 0x7fffffff) return CDL_ERR_ARG;
+    long long units = 0;
+    for (int j = 0; j < P.jobs; ++j) units += (long long)P.job[j].tiles_i * P.job[j].tiles_j * P.job[j].splits;
+    if (units > 0x3fffffff) return CDL_ERR_ARG;
     const int most = pair ? pair_slots[dev] : sms;
     P.slots = (int)(units < most ? units : most);
+    if (grad) spread_units(P);
     cfg.gridDim = dim3((pair ? 2u : 1u) * (unsigned)P.slots);
     cfg.stream = stream;
     cfg.numAttrs = pair ? 1 : 0;
-    void *args[5] = {&map_a, &map_b, &map_o, &map_f, &P};
-    if (cudaLaunchKernelExC(&cfg, variant(mode, pair, type), args) != cudaSuccess) {
+    void *args[2] = {&maps, &P};
+    if (cudaLaunchKernelExC(&cfg, variant(pair, grad, type), args) != cudaSuccess) {
         (void)cudaGetLastError();
         return CDL_ERR_LAUNCH;
     }
@@ -624,16 +798,18 @@ extern "C" int cdl_vocab_loss_fwd(const void *H, int64_t ldh, const void *W, int
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *base = static_cast<char *>(ws);
     LossParams P;
+    LossMaps maps;
     memset(&P, 0, sizeof P);
-    P.I = T;
-    P.J = V;
-    P.R = D;
+    memset(&maps, 0, sizeof maps);
     P.labels = reinterpret_cast<const long long *>(labels);
+    P.V = V;
     P.part = reinterpret_cast<float2 *>(base + kOffData);
     P.parts = p.parts;
     P.target = reinterpret_cast<float *>(base + p.off_target);
     P.status = static_cast<int *>(ws);
-    if ((rc = launch_product(STATS, type, H, ldh, W, ldw, nullptr, 0, nullptr, 0, P, st)) != CDL_OK) return rc;
+    const bool pair = T > 128;
+    if (!add_job(P, maps, type, pair, STATS, T, V, D, 1, H, ldh, W, ldw)) return CDL_ERR_LAUNCH;
+    if ((rc = launch_jobs(pair, false, type, maps, P, st)) != CDL_OK) return rc;
     loss_join_kernel<<<(unsigned)T, 128, 0, st>>>(P.part, p.parts, P.target, P.labels, V, loss, lse);
     return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
 }
@@ -663,44 +839,66 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
     }
     if (dH == nullptr && dW == nullptr) return CDL_OK;
     char *base = static_cast<char *>(ws);
-    LossParams P;
-    memset(&P, 0, sizeof P);
-    P.labels = reinterpret_cast<const long long *>(labels);
-    P.lse = lse;
-    P.dloss = dloss;
-    P.V = V;
-    P.status = static_cast<int *>(ws);
-    float *scale = reinterpret_cast<float *>(base + kOffScale);
-    loss_scale_kernel<<<1, 1024, 0, st>>>(dloss, P.labels, T, V, type == CDL_F16 ? 16384.0f : 1.0f, scale);
+    float *scale = reinterpret_cast<float *>(base + kOffScale), *acc = reinterpret_cast<float *>(base + p.off_acc);
+    loss_scale_kernel<<<1, 1024, 0, st>>>(dloss, reinterpret_cast<const long long *>(labels), T, V, type == CDL_F16 ? 16384.0f : 1.0f, scale);
     if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
-    P.scale = scale;
-    void *dl = base + kOffData;
-    P.acc = reinterpret_cast<float *>(base + p.off_acc);
-    P.acc_ld = p.acc_ld;
-    for (int k = 0; k < p.pieces; ++k) {
-        const int v0 = k * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
-        const char *Wk = static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2;
-        P.v0 = v0;
-        P.I = T;
-        P.J = words;
-        P.R = D;
-        if ((rc = launch_product(DLOGIT, type, H, ldh, Wk, ldw, dl, p.Vp, nullptr, 0, P, st)) != CDL_OK) return rc;
-        if (dW != nullptr) {
-            P.I = words;
-            P.J = D;
-            P.R = T;
-            if ((rc = launch_product(DW, type, dl, p.Vp, H, ldh, static_cast<char *>(dW) + (size_t)v0 * (size_t)lddw * 2, lddw, nullptr, 0, P, st)) != CDL_OK)
-                return rc;
+    LossParams P;
+    LossMaps maps;
+    // Launch k works on two pieces at a time: the products that read dl of piece k, and dl of piece k + 1 (into the other
+    // buffer).  One launch of mixed units has one ragged end where three would have three.
+    for (int k = -1; k < p.pieces; ++k) {
+        memset(&P, 0, sizeof P);
+        memset(&maps, 0, sizeof maps);
+        P.labels = reinterpret_cast<const long long *>(labels);
+        P.V = V;
+        P.lse = lse;
+        P.dloss = dloss;
+        P.scale = scale;
+        P.status = static_cast<int *>(ws);
+        P.acc = acc;
+        P.acc_ld = p.acc_ld;
+        P.acc_rows = p.acc_rows;
+        P.first = k == 0;
+        P.last = k == p.pieces - 1;
+        // (a TMA store fills the last 16-byte unit of a row with zeros beyond the output's columns: rows of a caller's
+        // matrix that do not end on one are stored by the threads)
+        P.out_tma = D % 8 == 0;
+        bool ok = true;
+        if (k >= 0) {
+            const int v0 = k * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
+            const void *dl = base + kOffData + (size_t)(k & 1) * p.dl_bytes;
+            if (dH != nullptr) {
+                const bool direct = P.last && p.splits == 1;
+                P.out_h = dH;
+                P.ldh = lddh;
+                ok = ok && add_job(P, maps, type, true, DH, T, D, words, p.splits, dl, p.Vp, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
+                ok = ok && (direct ? set_output(maps, P.jobs - 1, type, dH, (uint64_t)D, (uint64_t)T, lddh)
+                                   : set_output(maps, P.jobs - 1, CDL_F32, acc, (uint64_t)p.acc_ld, (uint64_t)p.splits * (uint64_t)p.acc_rows, p.acc_ld));
+            }
+            if (dW != nullptr) {
+                char *out = static_cast<char *>(dW) + (size_t)v0 * (size_t)lddw * 2;
+                P.out_w = out;
+                P.ldw = lddw;
+                ok = ok && add_job(P, maps, type, true, DW, words, D, T, 1, dl, p.Vp, H, ldh);
+                ok = ok && set_output(maps, P.jobs - 1, type, out, (uint64_t)D, (uint64_t)words, lddw);
+            }
         }
-        if (dH != nullptr) {
-            P.I = T;
-            P.J = D;
-            P.R = words;
-            P.first = k == 0;
-            P.last = k == p.pieces - 1;
-            if ((rc = launch_product(DH, type, dl, p.Vp, Wk, ldw, P.last ? dH : nullptr, lddh, P.last ? nullptr : P.acc, p.acc_ld, P, st)) != CDL_OK)
-                return rc;
+        if (k + 1 < p.pieces) {
+            const int v0 = (k + 1) * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
+            P.v0 = v0;
+            ok = ok && add_job(P, maps, type, true, DLOGIT, T, words, D, 1, H, ldh, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
+            ok = ok && set_output(maps, P.jobs - 1, type, base + kOffData + (size_t)((k + 1) & 1) * p.dl_bytes, (uint64_t)words, (uint64_t)T, p.Vp);
         }
+        if (!ok) return CDL_ERR_LAUNCH;
+        if ((rc = launch_jobs(true, true, type, maps, P, st)) != CDL_OK) return rc;
+    }
+    if (dH != nullptr && p.splits > 1) {
+        const long long units = (long long)T * ((D + 7) / 8);
+        const int blocks = (int)(units / 256 + 1 < 4096 ? units / 256 + 1 : 4096);
+        const long long step = (long long)p.acc_rows * p.acc_ld;
+        if (type == CDL_BF16) loss_sum_kernel<<<blocks, 256, 0, st>>>(acc, p.acc_ld, step, p.splits, T, D, scale, static_cast<__nv_bfloat16 *>(dH), lddh);
+        else loss_sum_kernel<<<blocks, 256, 0, st>>>(acc, p.acc_ld, step, p.splits, T, D, scale, static_cast<__half *>(dH), lddh);
+        if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
     }
     return CDL_OK;
 }

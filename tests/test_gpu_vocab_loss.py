@@ -102,6 +102,13 @@ def test_several_pieces_of_the_vocabulary(kind):
     check(torch, run(torch, h, w, y, gl, T, V, D, kind), h, w, y, gl, T, V, D, kind)
 
 
+def test_many_pieces_and_a_short_last_one():
+    import torch
+    T, V, D = 16500, 4200, 64                    # pieces of 2048 words: the last has 104
+    h, w, y, gl = problem(torch, T, V, D, "bf16", 4)
+    check(torch, run(torch, h, w, y, gl, T, V, D, "bf16"), h, w, y, gl, T, V, D, "bf16")
+
+
 def test_one_gradient_alone_is_the_same():
     import torch
     T, V, D = 200, 1500, 96
