@@ -230,15 +230,15 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         const uint32_t dst = scale_base + (q * (uint32_t)kGroup + (uint32_t)(kb - kg)) * (uint32_t)(slot_floats(BVEC) * 4);
                         const float *pa = P.sa + (long long)kb * P.M, *pb = P.sb + (long long)kb * P.nb;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = arow + i * 32 + lane;
-                            copy4_async(dst + (uint32_t)(i * 32 + lane) * 4u, r < P.M ? pa + r : P.sa, r < P.M);
+                        for (int j = 0; j < 4; ++j) {
+                            const int r = arow + j * 32 + lane;
+                            copy4_async(dst + (uint32_t)(j * 32 + lane) * 4u, r < P.M ? pa + r : P.sa, r < P.M);
                         }
                         if (BVEC) {
 #pragma unroll
-                            for (int i = 0; i < kTN / 32; ++i) {
-                                const int c = col + i * 32 + lane;
-                                copy4_async(dst + (uint32_t)(128 + i * 32 + lane) * 4u, c < P.N ? pb + c : P.sb, c < P.N);
+                            for (int j = 0; j < kTN / 32; ++j) {
+                                const int c = col + j * 32 + lane;
+                                copy4_async(dst + (uint32_t)(128 + j * 32 + lane) * 4u, c < P.N ? pb + c : P.sb, c < P.N);
                             }
                         } else if (lane < kTN / 128) {
                             const int c = (col >> 7) + lane;
@@ -517,6 +517,8 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
         else fill_bias_kernel<<<sms * 4, 256, 0, st>>>(static_cast<__half *>(out), ldo, M, N, bias);
         return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
     }
+    if (M <= kFewRowsFp8)
+        return launch_fp8_rows(A, lda, a_scale, B, ldb, b_scale, b_mode == CDL_FP8_ROWS, M, N, K, out, ldo, out_type, bias, static_cast<int *>(ws), st);
     Fp8Params P;
     memset(&P, 0, sizeof P);
     P.M = M;

@@ -106,6 +106,14 @@ struct NextQuant {
     int fast_div;       // as QuantDev::fast_div
 };
 
+// Forms of the language-model products for few rows (cdl_fp8_rows.cu, cdl_vocab_rows.cu).
+constexpr int kFewRowsFp8 = 2, kFewRowsLoss = 2;
+int launch_fp8_rows(const void *A, long long lda, const float *sa, const void *B, long long ldb, const float *sb, bool b_rows, int M, int N,
+                    int K, void *out, long long ldo, int out_type, const float *bias, int *status, cudaStream_t stream);
+int loss_rows_parts(int V);       // partial statistics per row
+int launch_loss_rows(const void *H, long long ldh, const void *W, long long ldw, int type, const long long *labels, int rows, int V, int D,
+                     float2 *part, int parts, float *target, int *status, cudaStream_t stream);
+
 // Tensor-core index GEMM (TMA + tcgen05 + TMEM); operands need 16-byte aligned bases and pitches.
 size_t tc_gemm_scratch_bytes(int I, int J, int R);
 int launch_index_gemm_tc(const GemmOperand &X, const GemmOperand &Y, int I, int J, int R, int32_t *acc_out,

@@ -198,8 +198,11 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             // kind looked up in every stage, 612 cycles a stage became 770).  K-major: one box of 64 reduced entries x the
             // block's rows.  MN-major: boxes of 64 rows x 64 reduced entries, the stored matrix's rows being the reduced
             // dimension.
+            // With one CTA per tile (few rows of H: bound by reading W) each tile begins at another place of the reduced
+            // dimension: a row pitch that is a power of two would have all CTAs read the same few memory channels at a time.
             auto stages_of = [&](auto a_mn, auto b_mn, const CUtensorMap *map_a, const CUtensorMap *map_b, int arow, int brow, int r0, int r1) {
-                for (int r = r0; r < r1; r += kBK) {
+                int r = PAIR ? r0 : brow / 256 * 5 % (r1 / kBK) * kBK;
+                for (int left = (r1 - r0) / kBK; left > 0; --left) {
                     const uint32_t fb = bar0 + 8u * st;
                     if (!mbar_try_wait_now(fb + kEmptyOff, par) && !mbar_wait(fb + kEmptyOff, par, abort_flag, kWaitNs)) {
                         failed = true;
@@ -215,6 +218,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 #pragma unroll
                         for (int b = 0; b < kBRows / 64; ++b) load(sb + (uint32_t)b * 8192u, map_b, brow + b * 64, r, fb);
                     } else load(sb, map_b, r, brow, fb);
+                    r += kBK;
+                    if (!PAIR && r == r1) r = 0;
                     if (++st == (uint32_t)kStages) {
                         st = 0u;
                         par ^= 1u;
@@ -498,9 +503,9 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 
 // One row per block: joins the tiles' maxima and sums, in a fixed order.
 __global__ void __launch_bounds__(128)
-loss_join_kernel(const float2 *__restrict__ part, int parts, const float *__restrict__ target, const long long *__restrict__ labels, int V,
-                 float *__restrict__ loss, float *__restrict__ lse)
+loss_join_kernel(const float2 *part, int parts, const float *target, const long long *labels, int V, float *loss, float *lse)
 {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float2 sh[4];
     const long long row = blockIdx.x;
     const float2 *p = part + row * parts;
@@ -623,7 +628,7 @@ constexpr int kPlanSlots = 74;                         // B200: planned for this
 LossPlan make_plan(int T, int V, int D)
 {
     LossPlan p;
-    p.parts = (int)(((long long)V + 127) / 128);
+    p.parts = T <= kFewRowsLoss ? loss_rows_parts(V) : (int)(((long long)V + 127) / 128);
     p.off_target = kOffData + up256((size_t)T * (size_t)p.parts * sizeof(float2));
     p.fwd_bytes = p.off_target + up256((size_t)T * sizeof(float));
     const long long words = tiles256(V);                // in units of 256
@@ -774,6 +779,25 @@ int launch_jobs(bool pair, bool grad, int type, LossMaps &maps, LossParams &P, c
     return CDL_OK;
 }
 
+// The join may be set up while the kernel before it drains (it waits for that kernel's results itself).
+int launch_join(const float2 *part, int parts, const float *target, const long long *labels, int T, int V, float *loss, float *lse, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)T);
+    cfg.blockDim = dim3(128);
+    cfg.stream = stream;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, loss_join_kernel, part, parts, target, labels, V, loss, lse) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CDL_ERR_LAUNCH;
+    }
+    return CDL_OK;
+}
+
 int check_common(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels, int32_t T, int32_t V, int32_t D)
 {
     if (T < 0 || V < 1 || D < 1 || (type != CDL_BF16 && type != CDL_F16)) return CDL_ERR_ARG;
@@ -810,6 +834,13 @@ extern "C" int cdl_vocab_loss_fwd(const void *H, int64_t ldh, const void *W, int
     if ((rc = check_device()) != CDL_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     char *base = static_cast<char *>(ws);
+    if (T <= kFewRowsLoss) {
+        float2 *part = reinterpret_cast<float2 *>(base + kOffData);
+        float *target = reinterpret_cast<float *>(base + p.off_target);
+        const long long *y = reinterpret_cast<const long long *>(labels);
+        if ((rc = launch_loss_rows(H, ldh, W, ldw, type, y, T, V, D, part, p.parts, target, static_cast<int *>(ws), st)) != CDL_OK) return rc;
+        return launch_join(part, p.parts, target, y, T, V, loss, lse, st);
+    }
     LossParams P;
     LossMaps maps;
     memset(&P, 0, sizeof P);
@@ -823,8 +854,7 @@ extern "C" int cdl_vocab_loss_fwd(const void *H, int64_t ldh, const void *W, int
     const bool pair = T > 128;
     if (!add_job(P, maps, type, pair, STATS, T, V, D, 1, H, ldh, W, ldw)) return CDL_ERR_LAUNCH;
     if ((rc = launch_jobs(pair, false, type, maps, P, st)) != CDL_OK) return rc;
-    loss_join_kernel<<<(unsigned)T, 128, 0, st>>>(P.part, p.parts, P.target, P.labels, V, loss, lse);
-    return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
+    return launch_join(P.part, p.parts, P.target, P.labels, T, V, loss, lse, st);
 }
 
 extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels,
