@@ -4,8 +4,9 @@
 //
 // What bounds it: 4 to 12 bytes of HBM per element, and close behind them the integer pipes: a Philox block is 20 wide
 // multiplies and 20 three-input logic operations for four elements.  One thread therefore handles eight consecutive
-// elements (two blocks, one or two 16-byte accesses per tensor), the comparison with p is one unsigned comparison of the
-// raw word, and the kept value, the scale and the residual are one fused multiply-add.
+// elements (two blocks, one or two 16-byte accesses per tensor) and fetches the next eight while it draws these; the comparison
+// with p is one unsigned comparison of the raw word, and the kept value, the scale and the residual are one fused
+// multiply-add under its predicate.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -21,51 +22,107 @@ struct DropoutDev {
     float scale;               // RN(1 / (1 - p))
     unsigned int threshold;    // a word w keeps its element when w >= threshold: (w >> 8) 2^-24 >= p
     int drop_all;              // p = 1: the threshold does not fit 32 bits
-    unsigned long long seed, first_index;
+    PhiloxKeys keys;
+    unsigned long long first_index;
 };
 
 template <bool RES>
 __device__ __forceinline__ float drop1(float x, float r, unsigned int w, const DropoutDev &d)
 {
-    // the element is selected before the product: a dropped infinity or NaN is gone
-    const float kept = (w >= d.threshold && !d.drop_all) ? x : 0.0f;
-    return RES ? fmaf(kept, d.scale, r) : kept * d.scale;
+    // (a dropped infinity or NaN is gone: the product is not taken)
+    float y = RES ? r : 0.0f;
+    if (w >= d.threshold && !d.drop_all) y = RES ? fmaf(x, d.scale, r) : x * d.scale;
+    return y;
 }
 
-// Eight elements per thread and step.  Every row starts at a multiple of 4 in the counter space and at a 16-byte
-// boundary of each tensor; cols is a multiple of 8 except for a single row, whose tail one more thread handles.
-template <typename T, bool RES>
-__global__ void __launch_bounds__(256)
-dropout_vec_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, long long cols, DropoutDev d)
-{
-    const long long octs = (cols + 7) >> 3;
-    const long long stride = (long long)gridDim.x * blockDim.x;
-    for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
-        const unsigned long long e_row = d.first_index + (unsigned long long)(r * cols);
-        for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < octs; i += stride) {
-            const long long c = i << 3;
-            const unsigned long long blk = (e_row + (unsigned long long)c) >> 2;
-            float v[8], q[8];
-            const bool whole = c + 8 <= cols;
-            if (whole) {
-                load8(x + r * ldx + c, v);
-                if (RES) load8(res + r * ldr + c, q);
-            } else {
+// Eight elements as they lie in memory: two or one 16-byte words.
+template <typename T>
+struct Oct {
+    uint4 q[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p)
+    {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = c + k < cols ? to_f32(x[r * ldx + c + k]) : 0.0f;
-                    if (RES) q[k] = c + k < cols ? to_f32(res[r * ldr + c + k]) : 0.0f;
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) q[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+    }
+    // elements 4 h .. 4 h + 3
+    __device__ __forceinline__ void half(int h, float (&v)[4]) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            v[0] = __uint_as_float(q[h].x);
+            v[1] = __uint_as_float(q[h].y);
+            v[2] = __uint_as_float(q[h].z);
+            v[3] = __uint_as_float(q[h].w);
+        } else {
+            unpack2(h ? q[0].z : q[0].x, v[0], v[1], T());
+            unpack2(h ? q[0].w : q[0].y, v[2], v[3], T());
+        }
+    }
+};
+
+// Eight elements per thread and step, the next step's loads on their way while this one's words are drawn.  Every row starts
+// at a multiple of 4 in the counter space and at a 16-byte boundary of each tensor; cols is a multiple of 8 except for a
+// single row, whose tail further threads handle.  A row is shorter than 2^28 elements: offsets are 32 bits.
+template <typename T, bool RES>
+__global__ void __launch_bounds__(256, 4)
+dropout_vec_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, unsigned int cols,
+                   const __grid_constant__ DropoutDev d)
+{
+    const unsigned int octs = cols >> 3, stride = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + threadIdx.x;
+    constexpr unsigned int kOct = 8u * sizeof(T);            // bytes
+    for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
+        const unsigned long long e_row = d.first_index + (unsigned long long)r * cols;
+        const char *xr = reinterpret_cast<const char *>(x + r * ldx), *qr = RES ? reinterpret_cast<const char *>(res + r * ldr) : nullptr;
+        char *yr = reinterpret_cast<char *>(y + r * ldy);
+        const unsigned long long blk0 = e_row >> 2;
+        unsigned int hi = (unsigned int)(blk0 >> 32);
+        unsigned long long head = philox_head(hi, d.keys);
+        Oct<T> xn, qn;
+        if (first < octs) {
+            xn.load(reinterpret_cast<const T *>(xr + first * kOct));
+            if (RES) qn.load(reinterpret_cast<const T *>(qr + first * kOct));
+        }
+        for (unsigned int i = first; i < octs; i += stride) {
+            const Oct<T> xc = xn, qc = qn;
+            if (i + stride < octs) {                         // (below 2^26: no wrap)
+                xn.load(reinterpret_cast<const T *>(xr + (i + stride) * kOct));
+                if (RES) qn.load(reinterpret_cast<const T *>(qr + (i + stride) * kOct));
+            }
+            const unsigned long long blk = blk0 + 2u * i;
+            if ((unsigned int)(blk >> 32) != hi) {
+                hi = (unsigned int)(blk >> 32);
+                head = philox_head(hi, d.keys);
+            }
+            uint4 out[sizeof(T) / 2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h == 1 && (unsigned int)blk == 0xffffffffu) head = philox_head(++hi, d.keys);
+                const uint4 a = philox4x32_10((unsigned int)blk + h, head, d.keys);
+                float v[4], q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                xc.half(h, v);
+                if (RES) qc.half(h, q);
+                v[0] = drop1<RES>(v[0], q[0], a.x, d);
+                v[1] = drop1<RES>(v[1], q[1], a.y, d);
+                v[2] = drop1<RES>(v[2], q[2], a.z, d);
+                v[3] = drop1<RES>(v[3], q[3], a.w, d);
+                if constexpr (sizeof(T) == 4) out[h] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                else if (h == 0) {
+                    out[0].x = pack2<T>(v[0], v[1]);
+                    out[0].y = pack2<T>(v[2], v[3]);
+                } else {
+                    out[0].z = pack2<T>(v[0], v[1]);
+                    out[0].w = pack2<T>(v[2], v[3]);
                 }
             }
-            const uint4 a = philox4x32_10(blk, d.seed), b = philox4x32_10(blk + 1, d.seed);
-            const unsigned int w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = drop1<RES>(v[k], RES ? q[k] : 0.0f, w[k], d);
-            if (whole) store8(y + r * ldy + c, v);
-            else
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (c + k < cols) y[r * ldy + c + k] = from_f32<T>(v[k]);
+            for (int k = 0; k < (int)sizeof(T) / 2; ++k) __stcs(reinterpret_cast<uint4 *>(yr + i * kOct) + k, out[k]);
+        }
+        if ((cols & 7u) != 0 && first < (cols & 7u)) {       // (a single row)
+            const unsigned int c = octs * 8u + first;
+            const unsigned long long e = e_row + c;
+            const uint4 a = philox4x32_10(e >> 2, d.keys);
+            const unsigned int k = (unsigned int)e & 3u, w = k == 0 ? a.x : (k == 1 ? a.y : (k == 2 ? a.z : a.w));
+            const T *xe = reinterpret_cast<const T *>(xr) + c, *qe = reinterpret_cast<const T *>(qr) + c;
+            reinterpret_cast<T *>(yr)[c] = from_f32<T>(drop1<RES>(to_f32(*xe), RES ? to_f32(*qe) : 0.0f, w, d));
         }
     }
 }
@@ -73,7 +130,7 @@ dropout_vec_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y,
 // Any alignment, pitch and first index: a thread takes the (up to four) elements of a row that share a Philox block.
 template <typename T, bool RES>
 __global__ void __launch_bounds__(256)
-dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, long long cols, DropoutDev d)
+dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, long long cols, const __grid_constant__ DropoutDev d)
 {
     const long long stride = (long long)gridDim.x * blockDim.x;
     for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
@@ -81,7 +138,7 @@ dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y,
         const int lead = (int)(e_row & 3u);
         const long long groups = (cols + lead + 3) >> 2;
         for (long long g = (long long)blockIdx.x * blockDim.x + threadIdx.x; g < groups; g += stride) {
-            const uint4 a = philox4x32_10((e_row >> 2) + (unsigned long long)g, d.seed);
+            const uint4 a = philox4x32_10((e_row >> 2) + (unsigned long long)g, d.keys);
             const unsigned int w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -95,7 +152,7 @@ dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y,
 
 template <typename T>
 int launch_typed(const void *xv, long long ldx, const void *rv, long long ldr, void *yv, long long ldy, long long rows, long long cols,
-                 const DropoutDev &d, cudaStream_t stream)
+                 DropoutDev d, cudaStream_t stream)
 {
     const T *x = static_cast<const T *>(xv), *res = static_cast<const T *>(rv);
     T *y = static_cast<T *>(yv);
@@ -107,28 +164,38 @@ int launch_typed(const void *xv, long long ldx, const void *rv, long long ldr, v
     auto aligned = [&](const void *p, long long ld) {
         return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows == 1 || (ld * (long long)sizeof(T)) % 16 == 0);
     };
-    const bool vec = (d.first_index & 3u) == 0 && (rows == 1 || cols % 8 == 0) && aligned(x, ldx) && aligned(y, ldy) &&
+    constexpr long long kMostCols = 1ll << 28;           // of a row of the vector form
+    const bool vec = (d.first_index & 3u) == 0 && (rows == 1 || (cols % 8 == 0 && cols < kMostCols)) && aligned(x, ldx) && aligned(y, ldy) &&
                      (res == nullptr || aligned(res, ldr));
     const int sms = sm_count();
     if (sms <= 0) return CDL_ERR_LAUNCH;
-    const long long per_row = vec ? (cols + 7) / 8 : (cols + 6) / 4;
     const int threads = 256;
-    const long long cap = (long long)sms * 8 * 4;
-    long long bx = (per_row + threads - 1) / threads;
-    if (bx > cap) bx = cap;
-    long long by = cap / bx;
-    if (by > rows) by = rows;
-    if (by > 65535) by = 65535;
-    if (by < 1) by = 1;
-    const dim3 grid((unsigned)bx, (unsigned)by);
-    if (vec) {
-        if (res != nullptr) dropout_vec_kernel<T, true><<<grid, threads, 0, stream>>>(x, ldx, res, ldr, y, ldy, rows, cols, d);
-        else dropout_vec_kernel<T, false><<<grid, threads, 0, stream>>>(x, ldx, res, ldr, y, ldy, rows, cols, d);
-    } else {
+    // (vector form: a grid that is resident at once, so that a thread has several steps to fetch ahead)
+    auto grid_for = [&](long long per_row, long long cap) {
+        long long bx = (per_row + threads - 1) / threads;
+        if (bx > cap) bx = cap;
+        if (bx < 1) bx = 1;
+        long long by = cap / bx;
+        if (by > rows) by = rows;
+        if (by > 65535) by = 65535;
+        return dim3((unsigned)bx, (unsigned)by);
+    };
+    if (!vec) {
+        const dim3 grid = grid_for((cols + 6) / 4, (long long)sms * 32);
         if (res != nullptr) dropout_any_kernel<T, true><<<grid, threads, 0, stream>>>(x, ldx, res, ldr, y, ldy, rows, cols, d);
         else dropout_any_kernel<T, false><<<grid, threads, 0, stream>>>(x, ldx, res, ldr, y, ldy, rows, cols, d);
+        return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
     }
-    if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
+    // a longer single row goes in several launches
+    const long long piece = rows == 1 ? kMostCols - 8 : cols;
+    for (long long c = 0; c < cols; c += piece) {
+        const long long n = cols - c < piece ? cols - c : piece;
+        const dim3 grid = grid_for((n + 7) / 8, (long long)sms * 4);
+        if (res != nullptr) dropout_vec_kernel<T, true><<<grid, threads, 0, stream>>>(x + c, ldx, res + c, ldr, y + c, ldy, rows, (unsigned)n, d);
+        else dropout_vec_kernel<T, false><<<grid, threads, 0, stream>>>(x + c, ldx, nullptr, ldr, y + c, ldy, rows, (unsigned)n, d);
+        if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
+        d.first_index += (unsigned long long)n;
+    }
     return CDL_OK;
 }
 
@@ -154,7 +221,7 @@ extern "C" int cdl_dropout(const void *x, int64_t ldx, const void *residual, int
     d.scale = d.drop_all ? 0.0f : (float)(1.0 / (1.0 - (double)p));
     d.threshold = d.drop_all ? 0xffffffffu : (unsigned int)ceil((double)p * 16777216.0) << 8;
     // (the largest p below 1 is 1 - 2^-24, whose threshold (2^24 - 1) << 8 fits)
-    d.seed = seed;
+    d.keys = philox_keys(seed);
     d.first_index = first_index;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     switch (type) {

@@ -117,3 +117,25 @@ def test_other_stream_and_empty():
     assert torch.equal(ref, y)
     assert cdl.cdl_dropout(None, 0, None, 0, None, 0, cdl.CDL_F32, 0, 5, 0.3, 9) == 0
     assert cdl.cdl_dropout(None, 0, None, 0, None, 0, cdl.CDL_F32, 5, 0, 0.3, 9) == 0
+
+
+def test_counter_word_carries_into_the_next():
+    """Blocks on both sides of a multiple of 2^32, at an even and at an odd place of a thread's two."""
+    import torch
+    for first in (4 * (2 ** 32 - 8), 4 * (2 ** 32 - 7), 4 * (5 * 2 ** 32 - 1), 4 * (2 ** 62 - 3)):
+        x = matrix(torch, 1, 256, 256, "float32", 11)
+        y = torch.empty_like(x)
+        cdl.cdl_dropout(x, 256, None, 0, y, 256, cdl.CDL_F32, 1, 256, 0.5, 3, first)
+        check(torch, y, x, None, kept(first, 1, 256, 3, 0.5), 0.5)
+
+
+def test_more_elements_than_one_launch_takes():
+    import torch
+    n = (1 << 28) + 1003                                  # a single row: two launches of the vector form
+    x = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    y = torch.empty_like(x)
+    cdl.cdl_dropout(x, n, None, 0, y, n, cdl.CDL_BF16, 1, n, 0.5, 21)
+    at = (1 << 28) - 2000
+    mask = torch.from_numpy(kept(at, 1, n - at, 21, 0.5)).cuda()[0]
+    assert torch.equal(y[at:] != 0, mask)
+    assert abs(float((y != 0).float().mean()) - 0.5) < 6 * 0.5 / n ** 0.5
