@@ -125,17 +125,11 @@ def load_library():
     lib.cdl_rescale_acc.argtypes = [P, I32, I64, C.c_float, C.c_float, P, P]
     lib.cdl_rescale_acc.restype = C.c_int
     lib.cdl_noalloc_status.restype = C.c_int
-    lib.cdl_dropout.argtypes = [P, I64, P, I64, P, I64, I32, I64, I64, C.c_float, C.c_uint64, C.c_uint64, P]
-    lib.cdl_fp8_quantize.argtypes = [P, I64, I32, I32, I32, I32, P, I64, P, P, I64, P, P]
-    lib.cdl_fp8_matmul.argtypes = [P, I64, P, P, I64, P, I32, I32, I32, I32, P, I64, I32, P, P, C.c_size_t, P]
     lib.cdl_fp8_matmul_workspace_bytes.argtypes = [I32, I32, I32]
     lib.cdl_fp8_matmul_workspace_bytes.restype = C.c_size_t
-    lib.cdl_vocab_loss_fwd.argtypes = [P, I64, P, I64, I32, P, I32, I32, I32, P, P, P, C.c_size_t, P]
-    lib.cdl_vocab_loss_bwd.argtypes = [P, I64, P, I64, I32, P, P, P, I32, I32, I32, P, I64, P, I64, P, C.c_size_t, P]
     lib.cdl_vocab_loss_workspace_bytes.argtypes = [I32, I32, I32, I32]
     lib.cdl_vocab_loss_workspace_bytes.restype = C.c_size_t
-    for name in ("cdl_dropout", "cdl_fp8_quantize", "cdl_fp8_matmul", "cdl_vocab_loss_fwd", "cdl_vocab_loss_bwd",
-                 "cdl_quantize_hard", "cdl_quantize_soft", "cdl_quantize_backward", "cdl_quantize_sample", "cdl_index_entropy",
+    for name in ("cdl_quantize_hard", "cdl_quantize_soft", "cdl_quantize_backward", "cdl_quantize_sample", "cdl_index_entropy",
                  "cdl_qlinear_fwd", "cdl_qlinear_bwd", "cdl_qlinear_bwd_dw_noalloc", "cdl_workspace_status",
                  "cdl_qconv_fwd", "cdl_qconv_bwd"):
         getattr(lib, name).restype = C.c_int
@@ -373,17 +367,36 @@ def cdl_rescale_acc(acc, acc_bits, n, q_x, q_y, out, stream=None, check=True):
     return _check(rc, "cdl_rescale_acc", check)
 
 
+_CALLS = None      # the compiled part of the binding, bound to the loaded library
+
+
+def _calls():
+    """_cdl_calls, which marshals the calls below (they run in microseconds; ctypes takes as long for their arguments)."""
+    global _CALLS
+    if _CALLS is None:
+        lib = load_library()
+        import torch
+        from . import _cdl_calls
+        raw = device = None
+        if torch.cuda.is_available():       # (no device: the call fails in the library, not here)
+            torch.cuda.init()
+            raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        at = [C.cast(getattr(lib, "cdl_" + name), C.c_void_p).value
+              for name in ("dropout", "fp8_quantize", "fp8_matmul", "vocab_loss_fwd", "vocab_loss_bwd")]
+        _cdl_calls.bind(raw, device, *at)
+        _CALLS = _cdl_calls
+    return _CALLS
+
+
 def cdl_dropout(x, ldx, residual, ldr, y, ldy, type, rows, cols, p, seed, first_index=0, stream=None, check=True):
     """Counter-based dropout (+ residual); the backward pass is the same call on the gradient with residual=None."""
-    rc = load_library().cdl_dropout(_ptr(x), ldx, _ptr(residual), ldr, _ptr(y), ldy, type, rows, cols, float(p), int(seed),
-                                    int(first_index), _stream(stream))
-    return _check(rc, "cdl_dropout", check)
+    rc = (_CALLS or _calls()).dropout(x, ldx, residual, ldr, y, ldy, type, rows, cols, p, seed, first_index, stream)
+    return _check(rc, "cdl_dropout", check) if rc else rc
 
 
 def cdl_fp8_quantize(x, ldx, type, rows, cols, mode, codes, ldc, scales, codes_t=None, ldt=0, scales_t=None, stream=None, check=True):
-    rc = load_library().cdl_fp8_quantize(_ptr(x), ldx, type, rows, cols, mode, _ptr(codes), ldc, _ptr(scales), _ptr(codes_t), ldt,
-                                         _ptr(scales_t), _stream(stream))
-    return _check(rc, "cdl_fp8_quantize", check)
+    rc = (_CALLS or _calls()).fp8_quantize(x, ldx, type, rows, cols, mode, codes, ldc, scales, codes_t, ldt, scales_t, stream)
+    return _check(rc, "cdl_fp8_quantize", check) if rc else rc
 
 
 def cdl_fp8_matmul_workspace_bytes(M, N, K) -> int:
@@ -392,9 +405,8 @@ def cdl_fp8_matmul_workspace_bytes(M, N, K) -> int:
 
 def cdl_fp8_matmul(A, lda, a_scale, B, ldb, b_scale, b_mode, M, N, K, out, ldo, out_type, bias=None, ws=None, ws_bytes=0, stream=None,
                    check=True):
-    rc = load_library().cdl_fp8_matmul(_ptr(A), lda, _ptr(a_scale), _ptr(B), ldb, _ptr(b_scale), b_mode, M, N, K, _ptr(out), ldo,
-                                       out_type, _ptr(bias), _ptr(ws), ws_bytes, _stream(stream))
-    return _check(rc, "cdl_fp8_matmul", check)
+    rc = (_CALLS or _calls()).fp8_matmul(A, lda, a_scale, B, ldb, b_scale, b_mode, M, N, K, out, ldo, out_type, bias, ws, ws_bytes, stream)
+    return _check(rc, "cdl_fp8_matmul", check) if rc else rc
 
 
 def cdl_vocab_loss_workspace_bytes(T, V, D, with_gradient) -> int:
@@ -402,13 +414,11 @@ def cdl_vocab_loss_workspace_bytes(T, V, D, with_gradient) -> int:
 
 
 def cdl_vocab_loss_fwd(H, ldh, W, ldw, type, labels, T, V, D, loss, lse, ws=None, ws_bytes=0, stream=None, check=True):
-    rc = load_library().cdl_vocab_loss_fwd(_ptr(H), ldh, _ptr(W), ldw, type, _ptr(labels), T, V, D, _ptr(loss), _ptr(lse), _ptr(ws),
-                                           ws_bytes, _stream(stream))
-    return _check(rc, "cdl_vocab_loss_fwd", check)
+    rc = (_CALLS or _calls()).vocab_loss_fwd(H, ldh, W, ldw, type, labels, T, V, D, loss, lse, ws, ws_bytes, stream)
+    return _check(rc, "cdl_vocab_loss_fwd", check) if rc else rc
 
 
 def cdl_vocab_loss_bwd(H, ldh, W, ldw, type, labels, lse, dloss, T, V, D, dH=None, lddh=0, dW=None, lddw=0, ws=None, ws_bytes=0,
                        stream=None, check=True):
-    rc = load_library().cdl_vocab_loss_bwd(_ptr(H), ldh, _ptr(W), ldw, type, _ptr(labels), _ptr(lse), _ptr(dloss), T, V, D, _ptr(dH),
-                                           lddh, _ptr(dW), lddw, _ptr(ws), ws_bytes, _stream(stream))
-    return _check(rc, "cdl_vocab_loss_bwd", check)
+    rc = (_CALLS or _calls()).vocab_loss_bwd(H, ldh, W, ldw, type, labels, lse, dloss, T, V, D, dH, lddh, dW, lddw, ws, ws_bytes, stream)
+    return _check(rc, "cdl_vocab_loss_bwd", check) if rc else rc

@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(256, 4)
 dropout_vec_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, unsigned int cols,
                    const __grid_constant__ DropoutDev d)
 {
+    follow_previous();
     const unsigned int octs = cols >> 3, stride = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + threadIdx.x;
     constexpr unsigned int kOct = 8u * sizeof(T);            // bytes
     for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
@@ -130,8 +131,10 @@ dropout_vec_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y,
 // Any alignment, pitch and first index: a thread takes the (up to four) elements of a row that share a Philox block.
 template <typename T, bool RES>
 __global__ void __launch_bounds__(256)
-dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, long long cols, const __grid_constant__ DropoutDev d)
+dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, long long cols,
+                   const __grid_constant__ DropoutDev d)
 {
+    follow_previous();
     const long long stride = (long long)gridDim.x * blockDim.x;
     for (long long r = blockIdx.y; r < rows; r += gridDim.y) {
         const unsigned long long e_row = d.first_index + (unsigned long long)(r * cols);
@@ -182,18 +185,17 @@ int launch_typed(const void *xv, long long ldx, const void *rv, long long ldr, v
     };
     if (!vec) {
         const dim3 grid = grid_for((cols + 6) / 4, (long long)sms * 32);
-        if (res != nullptr) dropout_any_kernel<T, true><<<grid, threads, 0, stream>>>(x, ldx, res, ldr, y, ldy, rows, cols, d);
-        else dropout_any_kernel<T, false><<<grid, threads, 0, stream>>>(x, ldx, res, ldr, y, ldy, rows, cols, d);
-        return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
+        return launch_following(res != nullptr ? &dropout_any_kernel<T, true> : &dropout_any_kernel<T, false>, grid, dim3(threads), 0, stream, x, ldx, res,
+                                ldr, y, ldy, rows, cols, (const DropoutDev)d);
     }
     // a longer single row goes in several launches
     const long long piece = rows == 1 ? kMostCols - 8 : cols;
     for (long long c = 0; c < cols; c += piece) {
         const long long n = cols - c < piece ? cols - c : piece;
         const dim3 grid = grid_for((n + 7) / 8, (long long)sms * 4);
-        if (res != nullptr) dropout_vec_kernel<T, true><<<grid, threads, 0, stream>>>(x + c, ldx, res + c, ldr, y + c, ldy, rows, (unsigned)n, d);
-        else dropout_vec_kernel<T, false><<<grid, threads, 0, stream>>>(x + c, ldx, nullptr, ldr, y + c, ldy, rows, (unsigned)n, d);
-        if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
+        const int rc = launch_following(res != nullptr ? &dropout_vec_kernel<T, true> : &dropout_vec_kernel<T, false>, grid, dim3(threads), 0, stream,
+                                        x + c, ldx, res != nullptr ? res + c : res, ldr, y + c, ldy, rows, (unsigned)n, (const DropoutDev)d);
+        if (rc != CDL_OK) return rc;
         d.first_index += (unsigned long long)n;
     }
     return CDL_OK;

@@ -139,6 +139,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     if (PAIR) cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_s;
+    follow_previous();
     bool failed = false;
     const uint32_t scale_base = smem_base + (uint32_t)(kStages * kStageBytes + kEpiWarps * kOutWarpBytes);
 
@@ -562,10 +563,12 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return CDL_ERR_LAUNCH;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.blockDim = dim3(kThreads);
     cfg.attrs = at;
     if (!attr_set[dev]) {
@@ -584,9 +587,10 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
                     return CDL_ERR_LAUNCH;
                 }
             }
-        at[0].val.clusterDim.x = 2;
+        at[1].val.clusterDim.x = 2;
         cfg.gridDim = dim3(2u * (unsigned)(sms / 2));
         cfg.dynamicSmemBytes = smem_bytes(false);
+        cfg.attrs = at + 1;
         cfg.numAttrs = 1;
         int n = 0;
         if (cudaOccupancyMaxActiveClusters(&n, variant(CDL_BF16, true, false), &cfg) != cudaSuccess || n < 1) {
@@ -599,11 +603,12 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     const int64_t units = (int64_t)P.tiles_i * P.tiles_j;
     const int64_t dev_slots = pair ? pair_slots[dev] : (P.splits > 1 ? units : sms);
     P.slots = (int)(units < dev_slots ? units : dev_slots);
-    at[0].val.clusterDim.x = pair ? 2u : (unsigned)P.splits;
+    at[1].val.clusterDim.x = pair ? 2u : (unsigned)P.splits;
+    cfg.attrs = at;
     cfg.gridDim = dim3((pair ? 2u : (unsigned)P.splits) * (unsigned)P.slots);
     cfg.dynamicSmemBytes = smem_bytes(bvec);
     cfg.stream = st;
-    cfg.numAttrs = pair || P.splits > 1 ? 1 : 0;
+    cfg.numAttrs = pair || P.splits > 1 ? 2 : 1;
     void *args[4] = {&map_a, &map_b, &map_o, &P};
     if (cudaLaunchKernelExC(&cfg, variant(out_type, pair, bvec), args) != cudaSuccess) {
         (void)cudaGetLastError();

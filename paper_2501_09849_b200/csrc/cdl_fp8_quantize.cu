@@ -159,6 +159,7 @@ quantize_fp8_kernel(const QuantFp8 Q)
     const int r0 = ti * 128, c0 = tj * 128;
     const int row = r0 + ty * 8, col = c0 + tx * 8;             // this thread's 8 x 8 piece
     const T *x = static_cast<const T *>(Q.x);
+    follow_previous();
 
     Piece<T> v;
     if (VEC && row + 8 <= Q.rows && col + 8 <= Q.cols) {
@@ -281,7 +282,7 @@ int launch_typed(const QuantFp8 &Q, bool blocks, cudaStream_t stream)
     const bool vec = (reinterpret_cast<uintptr_t>(Q.x) & 15u) == 0 && (Q.rows == 1 || (Q.ldx * (long long)sizeof(T)) % 16 == 0);
     const unsigned grid = (unsigned)Q.tiles_i * (unsigned)Q.tiles_j;
     const bool both = Q.codes_t != nullptr;
-#define CDL_GO(BL, BO, VE) quantize_fp8_kernel<T, BL, BO, VE><<<grid, kThreads, 0, stream>>>(Q)
+#define CDL_GO(BL, BO, VE) return launch_following(&quantize_fp8_kernel<T, BL, BO, VE>, dim3(grid), dim3(kThreads), 0, stream, Q)
     if (vec) {
         if (blocks) { if (both) CDL_GO(true, true, true); else CDL_GO(true, false, true); }
         else { if (both) CDL_GO(false, true, true); else CDL_GO(false, false, true); }
@@ -290,7 +291,6 @@ int launch_typed(const QuantFp8 &Q, bool blocks, cudaStream_t stream)
         else { if (both) CDL_GO(false, true, false); else CDL_GO(false, false, false); }
     }
 #undef CDL_GO
-    return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
 }
 
 }  // namespace

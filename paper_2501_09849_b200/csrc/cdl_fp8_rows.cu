@@ -65,7 +65,7 @@ __device__ __forceinline__ uint4 keep_codes(uint4 q, int live)
 
 template <int M, typename T>
 __global__ void __launch_bounds__(32 * kWarps, 1)
-fp8_rows_kernel(const RowsParams P)
+fp8_rows_kernel(RowsParams P)
 {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ __align__(8) unsigned long long bars[kWarps * kRingSlots];
@@ -78,6 +78,7 @@ fp8_rows_kernel(const RowsParams P)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    follow_previous();
     const int groups = kWarps / P.slices, slice = warp % P.slices, group = warp / P.slices;
     // a slice is a run of whole steps of 512 entries (16 per lane)
     const int steps = (P.K + 511) / 512;
@@ -184,9 +185,10 @@ fp8_rows_kernel(const RowsParams P)
     }
 }
 
+typedef void (*RowsKernel)(RowsParams);
 template <typename T>
-const void *variant(int M) { return M == 1 ? reinterpret_cast<const void *>(&fp8_rows_kernel<1, T>) : reinterpret_cast<const void *>(&fp8_rows_kernel<2, T>); }
-const void *variant(int M, int type)
+RowsKernel variant(int M) { return M == 1 ? &fp8_rows_kernel<1, T> : &fp8_rows_kernel<2, T>; }
+RowsKernel variant(int M, int type)
 {
     return type == CDL_F32 ? variant<float>(M) : (type == CDL_BF16 ? variant<__nv_bfloat16>(M) : variant<__half>(M));
 }
@@ -218,12 +220,7 @@ int launch_fp8_rows(const void *A, long long lda, const float *sa, const void *B
                 }
         attr_set[dev] = true;
     }
-    void *args[1] = {&P};
-    if (cudaLaunchKernel(variant(M, out_type), dim3((unsigned)grid), dim3(32 * kWarps), args, kRingSmem, stream) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return CDL_ERR_LAUNCH;
-    }
-    return CDL_OK;
+    return launch_following(variant(M, out_type), dim3((unsigned)grid), dim3(32 * kWarps), kRingSmem, stream, P);
 }
 
 }  // namespace cdl

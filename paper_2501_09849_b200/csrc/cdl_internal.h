@@ -106,6 +106,36 @@ struct NextQuant {
     int fast_div;       // as QuantDev::fast_div
 };
 
+// Launches of the language-model operators: a kernel may be set up while the one before it in the stream drains.  Every kernel
+// launched this way calls follow_previous() before its first access to memory that the stream's earlier work may touch;
+// what it is launched behind need not know.
+template <typename... Args>
+inline int launch_following(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return CDL_ERR_LAUNCH;
+    }
+    return CDL_OK;
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void follow_previous()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+#endif
+
 // Forms of the language-model products for few rows (cdl_fp8_rows.cu, cdl_vocab_rows.cu).
 constexpr int kFewRowsFp8 = 2, kFewRowsLoss = 2;
 int launch_fp8_rows(const void *A, long long lda, const float *sa, const void *B, long long ldb, const float *sb, bool b_rows, int M, int N,

@@ -184,6 +184,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
     if (PAIR) cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_s;
+    follow_previous();
     bool failed = false;
 
     if (warp == 0) {
@@ -505,8 +506,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 __global__ void __launch_bounds__(128)
 loss_join_kernel(const float2 *part, int parts, const float *target, const long long *labels, int V, float *loss, float *lse)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float2 sh[4];
+    follow_previous();
     const long long row = blockIdx.x;
     const float2 *p = part + row * parts;
     float m = -INFINITY, s = 0.0f;
@@ -540,9 +541,10 @@ loss_join_kernel(const float2 *part, int parts, const float *target, const long 
 // (measured on 777 x 32003 x 1000 in binary16: 3.9e-4 of dH's norm without it).  binary16 takes top = 2^14, so that
 // probabilities down to 2^-28 are normal numbers.
 __global__ void __launch_bounds__(1024)
-loss_scale_kernel(const float *__restrict__ dloss, const long long *__restrict__ labels, int T, int V, float top, float *__restrict__ out)
+loss_scale_kernel(const float *dloss, const long long *labels, int T, int V, float top, float *out)
 {
     __shared__ float sh[32];
+    follow_previous();
     float m = 0.0f;
     for (int t = threadIdx.x; t < T; t += 1024) {
         const long long y = labels[t];
@@ -568,9 +570,9 @@ loss_scale_kernel(const float *__restrict__ dloss, const long long *__restrict__
 // dH from the binary32 sums of the splits, added in their order
 template <typename T>
 __global__ void __launch_bounds__(256)
-loss_sum_kernel(const float *__restrict__ acc, long long acc_ld, long long split_elems, int splits, int rows, int cols,
-                const float *__restrict__ scale, T *__restrict__ out, long long ldo)
+loss_sum_kernel(const float *acc, long long acc_ld, long long split_elems, int splits, int rows, int cols, const float *scale, T *out, long long ldo)
 {
+    follow_previous();
     const float unscale = scale[1];
     const int per_row = (cols + 7) / 8;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)rows * per_row; i += (long long)gridDim.x * 256) {
@@ -639,11 +641,11 @@ LossPlan make_plan(int T, int V, int D)
     p.pieces = (int)((V + (long long)p.Vp - 1) / p.Vp);
     p.acc_ld = (long long)tiles256(D) * 256;
     p.acc_rows = tiles256(T) * 256;
-    // dH has few tiles, each as long as the piece: cut so that a part is at most a third of a slot's share of the launch
+    // dH has few tiles, each as long as the piece: cut so that a part is at most half of a slot's share of the launch
     const long long ti = tiles256(T), td = tiles256(D), wp = p.Vp / 256;
     const long long len_h = p.Vp / kBK, len_w = (T + kBK - 1) / kBK;
     const long long share = (ti * td * len_h + wp * td * len_w) / kPlanSlots + 1;
-    long long s = (3 * len_h + share - 1) / share;
+    long long s = (2 * len_h + share - 1) / share;
     if (s > len_h / 8) s = len_h / 8;
     if (s > kAccBytes / (4 * p.acc_rows * p.acc_ld + 1)) s = kAccBytes / (4 * p.acc_rows * p.acc_ld + 1);
     if (s > 16) s = 16;
@@ -737,14 +739,16 @@ int launch_jobs(bool pair, bool grad, int type, LossMaps &maps, LossParams &P, c
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return CDL_ERR_LAUNCH;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmemBytes;
-    cfg.attrs = at;
+    cfg.attrs = at + 1;
     if (!attr_set[dev]) {
         for (int v = 0; v < 8; ++v)
             if (cudaFuncSetAttribute(variant((v & 1) != 0, (v & 2) != 0, (v & 4) != 0 ? CDL_BF16 : CDL_F16), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) {
@@ -770,7 +774,8 @@ int launch_jobs(bool pair, bool grad, int type, LossMaps &maps, LossParams &P, c
     if (grad) spread_units(P);
     cfg.gridDim = dim3((pair ? 2u : 1u) * (unsigned)P.slots);
     cfg.stream = stream;
-    cfg.numAttrs = pair ? 1 : 0;
+    cfg.attrs = at;
+    cfg.numAttrs = pair ? 2 : 1;
     void *args[2] = {&maps, &P};
     if (cudaLaunchKernelExC(&cfg, variant(pair, grad, type), args) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -779,23 +784,9 @@ int launch_jobs(bool pair, bool grad, int type, LossMaps &maps, LossParams &P, c
     return CDL_OK;
 }
 
-// The join may be set up while the kernel before it drains (it waits for that kernel's results itself).
 int launch_join(const float2 *part, int parts, const float *target, const long long *labels, int T, int V, float *loss, float *lse, cudaStream_t stream)
 {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((unsigned)T);
-    cfg.blockDim = dim3(128);
-    cfg.stream = stream;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, loss_join_kernel, part, parts, target, labels, V, loss, lse) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return CDL_ERR_LAUNCH;
-    }
-    return CDL_OK;
+    return launch_following(&loss_join_kernel, dim3((unsigned)T), dim3(128), 0, stream, part, parts, target, labels, V, loss, lse);
 }
 
 int check_common(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels, int32_t T, int32_t V, int32_t D)
@@ -883,8 +874,9 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
     if (dH == nullptr && dW == nullptr) return CDL_OK;
     char *base = static_cast<char *>(ws);
     float *scale = reinterpret_cast<float *>(base + kOffScale), *acc = reinterpret_cast<float *>(base + p.off_acc);
-    loss_scale_kernel<<<1, 1024, 0, st>>>(dloss, reinterpret_cast<const long long *>(labels), T, V, type == CDL_F16 ? 16384.0f : 1.0f, scale);
-    if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
+    if ((rc = launch_following(&loss_scale_kernel, dim3(1), dim3(1024), 0, st, dloss, reinterpret_cast<const long long *>(labels), (int)T, (int)V,
+                               type == CDL_F16 ? 16384.0f : 1.0f, scale)) != CDL_OK)
+        return rc;
     LossParams P;
     LossMaps maps;
     // Launch k works on two pieces at a time: the products that read dl of piece k, and dl of piece k + 1 (into the other
@@ -939,9 +931,11 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
         const long long units = (long long)T * ((D + 7) / 8);
         const int blocks = (int)(units / 256 + 1 < 4096 ? units / 256 + 1 : 4096);
         const long long step = (long long)p.acc_rows * p.acc_ld;
-        if (type == CDL_BF16) loss_sum_kernel<<<blocks, 256, 0, st>>>(acc, p.acc_ld, step, p.splits, T, D, scale, static_cast<__nv_bfloat16 *>(dH), lddh);
-        else loss_sum_kernel<<<blocks, 256, 0, st>>>(acc, p.acc_ld, step, p.splits, T, D, scale, static_cast<__half *>(dH), lddh);
-        if (cudaGetLastError() != cudaSuccess) return CDL_ERR_LAUNCH;
+        if (type == CDL_BF16)
+            return launch_following(&loss_sum_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, (const float *)acc, p.acc_ld, step, p.splits,
+                                    (int)T, (int)D, (const float *)scale, static_cast<__nv_bfloat16 *>(dH), (long long)lddh);
+        return launch_following(&loss_sum_kernel<__half>, dim3((unsigned)blocks), dim3(256), 0, st, (const float *)acc, p.acc_ld, step, p.splits, (int)T, (int)D,
+                                (const float *)scale, static_cast<__half *>(dH), (long long)lddh);
     }
     return CDL_OK;
 }

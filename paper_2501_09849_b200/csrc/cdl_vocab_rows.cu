@@ -47,7 +47,6 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
     __shared__ __align__(8) unsigned long long bars[kWarps * kRingSlots];
     __shared__ float2 sh[kWarps][R];
     __shared__ int abort_s;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         abort_s = 0;
@@ -55,6 +54,7 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
+    follow_previous();
     Ring ringw;
     ringw.base = reinterpret_cast<const unsigned char *>(W);
     ringw.pitch = ldw * 2;
@@ -191,9 +191,8 @@ int launch_typed(const void *H, long long ldh, const void *W, long long ldw, con
         }
         attr_set[dev] = true;
     }
-    kernel<<<blocks, 32 * kWarps, kRingSmem, stream>>>(static_cast<const T *>(H), ldh, static_cast<const T *>(W), ldw, labels, rows, V, D,
-                                                       part, parts, target, status);
-    return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
+    return launch_following(kernel, dim3((unsigned)blocks), dim3(32 * kWarps), kRingSmem, stream, static_cast<const T *>(H), ldh,
+                            static_cast<const T *>(W), ldw, labels, rows, V, D, part, parts, target, status);
 }
 }  // namespace
 
