@@ -54,6 +54,10 @@ struct Fp8Params {
     int M, N, KB;                   // KB: blocks of 128 along the reduced dimension
     int tiles_i, tiles_j, slots;
     int splits;                     // CTAs of a cluster that share a tile (single-CTA tiles only)
+    // Pair tiles: the first `whole` units are whole tiles; the tiles behind them, too few to fill the device once more, are
+    // cut into tail_splits parts of the reduced dimension, whose sums go to `part`.
+    int whole, tail_splits;
+    float *part;                    // [unit - whole][64 groups of 4 columns][256 rows][4]
     int nb;                         // scales of a k-block of B: N, or ceil(N / 128)
     const float *sa, *sb, *bias;
     void *out;
@@ -109,9 +113,19 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t rank = PAIR || P.splits > 1 ? cluster_ctarank() : 0u;
     const int slot = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x / P.splits;
     const int split = PAIR ? 0 : (int)rank;
-    const int kb0 = PAIR ? 0 : (int)((long long)P.KB * split / P.splits);
-    const int kb1 = PAIR ? P.KB : (int)((long long)P.KB * (split + 1) / P.splits);
-    const int units = P.tiles_i * P.tiles_j;
+    const int units = PAIR ? P.whole + (P.tiles_i * P.tiles_j - P.whole) * P.tail_splits : P.tiles_i * P.tiles_j;
+    // the tile and the k-blocks of a unit
+    auto unit_at = [&](int u, int &ti, int &tj, int &kb0, int &kb1) {
+        int tile = u, part = split, parts = PAIR ? 1 : P.splits;
+        if (PAIR && u >= P.whole) {
+            parts = P.tail_splits;
+            tile = P.whole + (u - P.whole) / parts;
+            part = (u - P.whole) - (tile - P.whole) * parts;
+        }
+        tile_at(tile, P.tiles_i, P.tiles_j, ti, tj);
+        kb0 = parts == 1 ? 0 : (int)((long long)P.KB * part / parts);
+        kb1 = parts == 1 ? P.KB : (int)((long long)P.KB * (part + 1) / parts);
+    };
 
     const uint32_t bar0 = smem_u32(&bars[0]);
     constexpr uint32_t kEmptyOff = 8u * kStagesMax;
@@ -150,8 +164,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (lane == 0) {
                 uint32_t st = 0u, par = 1u;
                 for (int u = slot; u < units && !failed; u += P.slots) {
-                    int ti, tj;
-                    tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+                    int ti, tj, kb0, kb1;
+                    unit_at(u, ti, tj, kb0, kb1);
                     const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
                     const int brow = tj * kTN + (PAIR ? (int)rank * 128 : 0);
                     for (int kb = kb0; kb < kb1; ++kb) {
@@ -185,6 +199,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const uint32_t idesc = (1u << 4) | ((uint32_t)(kTN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
                 uint32_t st = 0u, par = 0u, buf = 0u, tpar = 1u;
                 for (int u = slot; u < units && !failed; u += P.slots) {
+                    int ti, tj, kb0, kb1;
+                    unit_at(u, ti, tj, kb0, kb1);
                     for (int kb = kb0; kb < kb1; ++kb) {
                         const uint32_t fb = bar0 + 8u * st, tf = tfull0 + 8u * buf, te = tempty0 + 8u * buf;
                         if ((!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs)) ||
@@ -218,8 +234,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             // asynchronous 4-byte copies (their addresses have no alignment to rely on), several stages ahead
             uint32_t q = 0u, par = 1u;
             for (int u = slot; u < units && !failed; u += P.slots) {
-                int ti, tj;
-                tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+                int ti, tj, kb0, kb1;
+                unit_at(u, ti, tj, kb0, kb1);
                 const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0), col = tj * kTN;
                 for (int kg = kb0; kg < kb1; kg += kGroup) {
                     const uint32_t sf = sfull0 + 8u * q;
@@ -264,8 +280,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const uint32_t wbuf = smem_base + (uint32_t)(kStages * kStageBytes) + (uint32_t)((warp - 4) * kOutWarpBytes);
         uint32_t buf = 0u, tpar = 0u, q = 0u, spar = 0u, oblk = 0u;
         for (int u = slot; u < units && !failed; u += P.slots) {
-            int ti, tj;
-            tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+            int ti, tj, kb0, kb1;
+            unit_at(u, ti, tj, kb0, kb1);
             const int row0 = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
             const int row = row0 + lane;
 #pragma unroll
@@ -366,6 +382,13 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 break;
             }
             if (row0 >= P.M) continue;
+            if (PAIR && u >= P.whole) {
+                // a part of a tile: its sums as they are, four columns of 32 consecutive rows per instruction
+                float4 *q = reinterpret_cast<float4 *>(P.part) + ((long long)(u - P.whole) * 64 + group * (kCols / 4)) * 256 + (int)rank * 128 + quarter * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < kCols / 4; ++j) q[j * 256] = make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
+                continue;
+            }
 #pragma unroll
             for (int ch = 0; ch < kCols / 32; ++ch) {
                 const int col0 = tj * kTN + tile_col(ch);
@@ -378,42 +401,57 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         if (col0 + 2 * j + 1 < P.N) a[j].y += __ldg(P.bias + col0 + 2 * j + 1);
                     }
                 }
-                if (P.out_tma) {
-                    // 64-byte pieces of the warp's 32 rows through its staging block (64-byte swizzle): TMA clips at the edges
-                    constexpr int kPiece = 64 / (int)sizeof(T);
+                // 64-byte pieces of the warp's 32 rows through its staging block (64-byte swizzle), then by TMA (which clips at the
+                // edges), or, where rows do not start and end on 16 bytes, copied out row by row: consecutive lanes on
+                // consecutive entries (with a row per lane instead, 3000 x 1500 x 5008 took 70 us)
+                constexpr int kPiece = 64 / (int)sizeof(T);
 #pragma unroll
-                    for (int pc = 0; pc < 32 / kPiece; ++pc) {
-                        if (col0 + pc * kPiece >= P.N) break;
-                        if (lane == 0) bulk_wait_read<kOutBlocks - 1>();     // the store that last used this block has read it
-                        __syncwarp();
-                        const uint32_t src = wbuf + oblk, dst = src + (uint32_t)lane * 64u;
+                for (int pc = 0; pc < 32 / kPiece; ++pc) {
+                    const int c0 = col0 + pc * kPiece;
+                    if (c0 >= P.N) break;
+                    if (lane == 0) bulk_wait_read<kOutBlocks - 1>();     // the store that last used this block has read it
+                    __syncwarp();
+                    const uint32_t src = wbuf + oblk, dst = src + (uint32_t)lane * 64u;
 #pragma unroll
-                        for (int c4 = 0; c4 < 4; ++c4) {
-                            uint32_t w[4];
+                    for (int c4 = 0; c4 < 4; ++c4) {
+                        uint32_t w[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if constexpr (sizeof(T) == 4) w[j] = __float_as_uint((j & 1) ? a[pc * 8 + c4 * 2 + (j >> 1)].y : a[pc * 8 + c4 * 2 + (j >> 1)].x);
-                                else w[j] = pack2<T>(a[c4 * 4 + j].x, a[c4 * 4 + j].y);
-                            }
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c4 ^ ((lane >> 1) & 3)) << 4)),
-                                         "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                                         : "memory");
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (sizeof(T) == 4) w[j] = __float_as_uint((j & 1) ? a[pc * 8 + c4 * 2 + (j >> 1)].y : a[pc * 8 + c4 * 2 + (j >> 1)].x);
+                            else w[j] = pack2<T>(a[c4 * 4 + j].x, a[c4 * 4 + j].y);
                         }
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c4 ^ ((lane >> 1) & 3)) << 4)),
+                                     "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                                     : "memory");
+                    }
+                    if (P.out_tma) {
                         fence_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            tma_store_2d(&map_o, col0 + pc * kPiece, row0, src);
+                            tma_store_2d(&map_o, c0, row0, src);
                             bulk_commit();
                         }
-                        oblk = oblk + (uint32_t)kOutBytes == (uint32_t)kOutWarpBytes ? 0u : oblk + (uint32_t)kOutBytes;
+                    } else {
+                        __syncwarp();
+                        constexpr int kAtOnce = 32 / kPiece;             // rows of an instruction
+                        const int c = lane % kPiece;
+                        const uint32_t unit = (uint32_t)(c * (int)sizeof(T)) >> 4, in = (uint32_t)(c * (int)sizeof(T)) & 15u;
+#pragma unroll 4
+                        for (int r = lane / kPiece; r < 32; r += kAtOnce) {
+                            const uint32_t at = src + (uint32_t)r * 64u + ((unit ^ (((uint32_t)r >> 1) & 3u)) << 4) + in;
+                            if (row0 + r < P.M && c0 + c < P.N) {
+                                T *o = static_cast<T *>(P.out) + (long long)(row0 + r) * P.ldo + c0 + c;
+                                if constexpr (sizeof(T) == 4) *o = lds32(at);
+                                else {
+                                    unsigned short h;
+                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
+                                    *reinterpret_cast<unsigned short *>(o) = h;
+                                }
+                            }
+                        }
+                        __syncwarp();
                     }
-                } else if (row < P.M) {
-                    T *o = static_cast<T *>(P.out) + (long long)row * P.ldo + col0;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        if (col0 + 2 * j < P.N) o[2 * j] = from_f32<T>(a[j].x);
-                        if (col0 + 2 * j + 1 < P.N) o[2 * j + 1] = from_f32<T>(a[j].y);
-                    }
+                    oblk = oblk + (uint32_t)kOutBytes == (uint32_t)kOutWarpBytes ? 0u : oblk + (uint32_t)kOutBytes;
                 }
             }
         }
@@ -477,6 +515,34 @@ const void *variant(int type, bool pair, bool bvec)
     return type == CDL_BF16 ? variant<__nv_bfloat16>(pair, bvec) : variant<__half>(pair, bvec);
 }
 
+// The tiles that were cut into parts: the parts' sums in their order, the bias, the output type.  One thread per four columns of
+// a row, consecutive threads on consecutive rows (as the parts are stored).
+template <typename T>
+__global__ void __launch_bounds__(256)
+fp8_sum_kernel(const float *part, int parts, int first, int tiles_i, int tiles_j, int M, int N, const float *bias, T *out, long long ldo)
+{
+    follow_previous();
+    int ti, tj;
+    tile_at(first + (int)blockIdx.x, tiles_i, tiles_j, ti, tj);
+    const long long row = (long long)ti * 256 + threadIdx.x;
+    const int col = tj * 256 + (int)blockIdx.y * 4;
+    if (row >= M || col >= N) return;
+    const float4 *q = reinterpret_cast<const float4 *>(part) + ((long long)blockIdx.x * parts * 64 + blockIdx.y) * 256 + threadIdx.x;
+    float4 v = q[0];
+    for (int s = 1; s < parts; ++s) {
+        const float4 w = q[(long long)s * 64 * 256];
+        v.x += w.x;
+        v.y += w.y;
+        v.z += w.z;
+        v.w += w.w;
+    }
+    const float o4[4] = {v.x, v.y, v.z, v.w};
+    T *o = out + row * ldo + col;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (col + j < N) o[j] = from_f32<T>(o4[j] + (bias != nullptr ? __ldg(bias + col + j) : 0.0f));
+}
+
 // out = bias (or 0) where the reduced dimension is empty
 template <typename T>
 __global__ void fill_bias_kernel(T *out, long long ldo, long long M, int N, const float *bias)
@@ -488,9 +554,63 @@ __global__ void fill_bias_kernel(T *out, long long ldo, long long M, int N, cons
 }  // namespace
 }  // namespace cdl
 
+namespace {
+// What a product of these sizes runs as.  Planned for a B200's 148 SMs so that workspace sizes are fixed.
+struct Fp8Plan {
+    bool pair;
+    int tiles_i, tiles_j;
+    int splits;                 // CTAs of a cluster per tile (single-CTA tiles)
+    int whole, tail_splits;     // pair tiles: see Fp8Params
+    size_t part_bytes;
+};
+constexpr int kPlanSms = 148;
+constexpr size_t kStatusBytes = 256;
+
+bool make_plan(int32_t M, int32_t N, int32_t K, Fp8Plan *p)
+{
+    const int64_t KB = ((int64_t)K + 127) / 128, pairs = kPlanSms / 2;
+    const int64_t pair_tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256), tiles = (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128);
+    if (tiles > 0x3fffffff) return false;
+    // Single-CTA tiles: few of them are cut over the CTAs of a cluster.  (Clusters of four and eight do not fit everywhere: the
+    // device runs 32 and 14 of them at once for certain.)
+    int64_t splits = 1;
+    const int64_t clusters[4] = {kPlanSms, pairs, 32, 14};
+    for (int i = 1; i < 4 && tiles <= clusters[i] && (2ll << i) <= KB; ++i) splits = 1ll << i;
+    // Whichever form is estimated to be faster, in nanoseconds: a start, a stage (550 and 420: a pair's stage does four times the
+    // work), a tile's output, the sum over a cluster.  Measured both ways: 512 x 4096 x 4096 21.2 us in pairs against 17.5,
+    // 1009 x 2304 x 1000 9.3 against 7.6, 2048 x 2048 x 2048 14.3 against 17.7, 6000 x 3000 x 2000 46.9 against 61.8.
+    const int64_t pair_rounds = (pair_tiles + pairs - 1) / pairs, rounds = splits > 1 ? 1 : (tiles + kPlanSms - 1) / kPlanSms;
+    const int64_t pair_ns = 5000 + pair_rounds * (1200 + 550 * KB), single_ns = 4000 + rounds * (800 + 420 * ((KB + splits - 1) / splits)) + (splits > 1 ? 2000 : 0);
+    p->pair = pair_ns < single_ns;
+    const int edge = p->pair ? 256 : 128;
+    p->tiles_i = (int)(((int64_t)M + edge - 1) / edge);
+    p->tiles_j = (int)(((int64_t)N + edge - 1) / edge);
+    p->splits = p->pair ? 1 : (int)splits;
+    p->tail_splits = 1;
+    p->whole = (int)pair_tiles;
+    p->part_bytes = 0;
+    if (!p->pair || pair_tiles < pairs) return true;
+    // The last, partly filled round: cut its tiles so that the parts fill the device.  A stage takes half a microsecond and the
+    // parts cost their way through memory and a launch, about as much as 24 stages (2304 x 4608 x 50176: 14 tiles of the last
+    // round in 5 parts each, 858 -> 716 us; 2304 x 2304 x 4608, 36 stages, 43 us either way).
+    const int64_t tail = pair_tiles % pairs;
+    if (tail > 0) {
+        const int64_t s = pairs / tail;
+        if (s >= 2 && KB - KB / s >= 32) {
+            p->tail_splits = (int)s;
+            p->whole = (int)(pair_tiles - tail);
+            p->part_bytes = (size_t)tail * (size_t)s * 256 * 256 * sizeof(float);
+        }
+    }
+    return true;
+}
+}  // namespace
+
 extern "C" size_t cdl_fp8_matmul_workspace_bytes(int32_t M, int32_t N, int32_t K)
 {
-    return M < 0 || N < 0 || K < 0 ? 0 : 256;           // the status block
+    Fp8Plan p;
+    if (M < 0 || N < 0 || K < 0) return 0;
+    return make_plan(M, N, K, &p) ? kStatusBytes + p.part_bytes : kStatusBytes;      // the status block, the parts of cut tiles
 }
 
 extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, const void *B, int64_t ldb, const float *b_scale,
@@ -533,19 +653,15 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     P.out = out;
     P.ldo = ldo;
     P.status = static_cast<int *>(ws);
-    const int64_t pair_tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
-    const int64_t tiles = (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128);
-    if (tiles > 0x3fffffff) return CDL_ERR_ARG;
-    const bool pair = pair_tiles >= sms / 2;
-    P.tiles_i = pair ? (M + 255) / 256 : (M + 127) / 128;
-    P.tiles_j = pair ? (N + 255) / 256 : (N + 127) / 128;
-    P.splits = 1;
-    if (!pair) {
-        int64_t s = sms / tiles;
-        if (s > P.KB / 2) s = P.KB / 2;
-        if (s > kMaxSplits) s = kMaxSplits;
-        while (P.splits * 2 <= s) P.splits *= 2;        // powers of two: they fill a GPC's SMs
-    }
+    Fp8Plan plan;
+    if (!make_plan(M, N, K, &plan)) return CDL_ERR_ARG;
+    const bool pair = plan.pair;
+    P.tiles_i = plan.tiles_i;
+    P.tiles_j = plan.tiles_j;
+    P.splits = plan.splits;
+    P.whole = plan.whole;
+    P.tail_splits = plan.tail_splits;
+    P.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kStatusBytes);
     const int esz = type_bytes(out_type);
     // (a TMA store fills the last 16-byte unit of a row with zeros beyond N: rows that do not end on one are stored directly)
     P.out_tma = P.splits == 1 && (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && (ldo * esz) % 16 == 0 && ((int64_t)N * esz) % 16 == 0;
@@ -600,7 +716,8 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
         pair_slots[dev] = n < sms / 2 ? n : sms / 2;
         attr_set[dev] = true;
     }
-    const int64_t units = (int64_t)P.tiles_i * P.tiles_j;
+    const int64_t tiles = (int64_t)P.tiles_i * P.tiles_j;
+    const int64_t units = pair ? P.whole + (tiles - P.whole) * P.tail_splits : tiles;
     const int64_t dev_slots = pair ? pair_slots[dev] : (P.splits > 1 ? units : sms);
     P.slots = (int)(units < dev_slots ? units : dev_slots);
     at[1].val.clusterDim.x = pair ? 2u : (unsigned)P.splits;
@@ -613,6 +730,18 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     if (cudaLaunchKernelExC(&cfg, variant(out_type, pair, bvec), args) != cudaSuccess) {
         (void)cudaGetLastError();
         return CDL_ERR_LAUNCH;
+    }
+    if (P.tail_splits > 1) {
+        const dim3 grid((unsigned)(tiles - P.whole), 64);
+        const float *part = P.part;
+        if (out_type == CDL_F32)
+            return launch_following(&fp8_sum_kernel<float>, grid, dim3(256), 0, st, part, P.tail_splits, P.whole, P.tiles_i, P.tiles_j, (int)M, (int)N, bias,
+                                    static_cast<float *>(out), (long long)ldo);
+        if (out_type == CDL_BF16)
+            return launch_following(&fp8_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, part, P.tail_splits, P.whole, P.tiles_i, P.tiles_j, (int)M, (int)N,
+                                    bias, static_cast<__nv_bfloat16 *>(out), (long long)ldo);
+        return launch_following(&fp8_sum_kernel<__half>, grid, dim3(256), 0, st, part, P.tail_splits, P.whole, P.tiles_i, P.tiles_j, (int)M, (int)N, bias,
+                                static_cast<__half *>(out), (long long)ldo);
     }
     return CDL_OK;
 }

@@ -148,13 +148,14 @@ def run_matmul(torch, M, N, K, mode, out, bias=None, pad=0, seed=0, offset=0, st
     (33, 1000, 1111, 0, 1, "bf16"), (64, 512, 2048, 8, 0, "f16"), (128, 256, 384, 0, 0, "f32"), (129, 300, 640, 0, 0, "bf16"),
     (1009, 2304, 1000, 0, 0, "f16"), (300, 4000, 272, 0, 0, "f32"), (2304, 2304, 512, 0, 0, "f32"), (2300, 2310, 640, 2, 0, "bf16"),
     (2561, 2001, 144, 0, 1, "f16"), (4000, 1500, 129, 0, 0, "f32"), (3001, 5003, 130, 0, 0, "bf16"),
+    (2304, 2304, 9000, 0, 0, "f32"), (2301, 2303, 8300, 1, 0, "bf16"), (4800, 1100, 6200, 0, 0, "f16"),      # the last round's tiles in parts
 ])
 def test_product(mode, M, N, K, pad, offset, out):
     import torch
     run_matmul(torch, M, N, K, mode, out, pad=pad, seed=M + N + K, offset=offset)
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 300, 1024), (200, 300, 256), (2500, 2500, 256)])
+@pytest.mark.parametrize("M,N,K", [(1, 300, 1024), (2, 77, 513), (200, 300, 256), (2500, 2500, 256), (2304, 2304, 8192)])
 def test_product_with_bias(M, N, K):
     import torch
     bias = torch.randn(N, generator=torch.Generator().manual_seed(3)) * 3
