@@ -51,6 +51,7 @@ constexpr int kMaxSlots = 80;                          // CTA pairs of a launch 
 struct LossJob {
     int mode;
     int I, J, R;
+    int tn;                         // columns of a tile: 256, or fewer where there are few tiles (STATS, DLOGIT)
     int tiles_i, tiles_j, splits;
     // Backward: its units (tile, split) on the launch's slots: slot s takes units i * slots + s for i < rounds, then extra[s] .. extra[s + 1] - 1.
     int rounds;
@@ -152,9 +153,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
     __shared__ uint32_t tmem_base_s;
     __shared__ int abort_s;
 
-    constexpr int kBRows = PAIR ? 128 : 256;           // columns of the tile that this CTA stages
-    constexpr uint32_t kBBytes = (uint32_t)kBRows * 128u;
-    constexpr uint32_t kStageBytes = (uint32_t)kBlockBytes + kBBytes;
+    constexpr int kBRows = PAIR ? 128 : 256;           // most columns of a tile that this CTA stages
+    constexpr uint32_t kStageBytes = (uint32_t)kBlockBytes + (uint32_t)kBRows * 128u;
     constexpr int kStages = PAIR ? 6 : 4;
     static_assert(kStages * kStageBytes <= kStagesMax * 2 * kBlockBytes, "shared memory");
     const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
@@ -201,8 +201,9 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             // dimension.
             // With one CTA per tile (few rows of H: bound by reading W) each tile begins at another place of the reduced
             // dimension: a row pitch that is a power of two would have all CTAs read the same few memory channels at a time.
-            auto stages_of = [&](auto a_mn, auto b_mn, const CUtensorMap *map_a, const CUtensorMap *map_b, int arow, int brow, int r0, int r1) {
-                int r = PAIR ? r0 : brow / 256 * 5 % (r1 / kBK) * kBK;
+            auto stages_of = [&](auto a_mn, auto b_mn, const CUtensorMap *map_a, const CUtensorMap *map_b, int arow, int brow, uint32_t bytes,
+                                 int r0, int r1) {
+                int r = PAIR ? r0 : brow / 64 * 5 % (r1 / kBK) * kBK;
                 for (int left = (r1 - r0) / kBK; left > 0; --left) {
                     const uint32_t fb = bar0 + 8u * st;
                     if (!mbar_try_wait_now(fb + kEmptyOff, par) && !mbar_wait(fb + kEmptyOff, par, abort_flag, kWaitNs)) {
@@ -210,7 +211,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                         return;
                     }
                     const uint32_t sa = smem_base + st * kStageBytes, sb = sa + kBlockBytes;
-                    if (!PAIR || rank == 0) mbar_expect_tx(fb, (PAIR ? 2u : 1u) * kStageBytes);
+                    if (!PAIR || rank == 0) mbar_expect_tx(fb, bytes);
                     if (decltype(a_mn)::value) {
                         load(sa, map_a, arow, r, fb);
                         load(sa + 8192u, map_a, arow + 64, r, fb);
@@ -234,10 +235,11 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                 const int mode = GRAD ? P.job[u.j].mode : STATS;
                 const CUtensorMap *map_a = &maps.a[u.j], *map_b = &maps.b[u.j];
                 const int arow = u.ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
-                const int brow = u.tj * 256 + (PAIR ? (int)rank * 128 : 0);
-                if (GRAD && mode == DW) stages_of(Yes(), Yes(), map_a, map_b, arow, brow, u.rb0 * kBK, u.rb1 * kBK);
-                else if (GRAD && mode == DH) stages_of(No(), Yes(), map_a, map_b, arow, brow, u.rb0 * kBK, u.rb1 * kBK);
-                else stages_of(No(), No(), map_a, map_b, arow, brow, u.rb0 * kBK, u.rb1 * kBK);
+                const int brows = PAIR ? P.job[u.j].tn / 2 : P.job[u.j].tn, brow = u.tj * P.job[u.j].tn + (PAIR ? (int)rank * brows : 0);
+                const uint32_t bytes = (PAIR ? 2u : 1u) * ((uint32_t)kBlockBytes + (uint32_t)brows * 128u);      // of a stage, of both CTAs of a pair
+                if (GRAD && mode == DW) stages_of(Yes(), Yes(), map_a, map_b, arow, brow, bytes, u.rb0 * kBK, u.rb1 * kBK);
+                else if (GRAD && mode == DH) stages_of(No(), Yes(), map_a, map_b, arow, brow, bytes, u.rb0 * kBK, u.rb1 * kBK);
+                else stages_of(No(), No(), map_a, map_b, arow, brow, bytes, u.rb0 * kBK, u.rb1 * kBK);
             }
         }
     } else if (warp == 1) {
@@ -248,12 +250,12 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             const uint64_t k_d = make_desc(smem_base, 16, 1024), mn_d = make_desc(smem_base, 8192, 1024);
             const uint32_t d_hi = (uint32_t)(k_d >> 32), k_lo = (uint32_t)k_d, mn_lo = (uint32_t)mn_d;      // (the upper words agree)
             constexpr uint32_t kFmt = __is_same(T, __nv_bfloat16) ? 1u : 0u;
-            const uint32_t idesc0 = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((256u >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
+            const uint32_t idesc0 = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
             uint32_t st = 0u, par = 0u, buf = 0u, tpar = 1u;
-            auto stages_of = [&](auto a_mn, auto b_mn, int count) {
+            auto stages_of = [&](auto a_mn, auto b_mn, int tn, int count) {
                 constexpr bool kA = decltype(a_mn)::value, kB = decltype(b_mn)::value;
                 const uint32_t a_lo0 = kA ? mn_lo : k_lo, b_lo0 = (kB ? mn_lo : k_lo) + (uint32_t)(kBlockBytes >> 4);
-                const uint32_t idesc = idesc0 | ((kA ? 1u : 0u) << 15) | ((kB ? 1u : 0u) << 16);
+                const uint32_t idesc = idesc0 | ((kA ? 1u : 0u) << 15) | ((kB ? 1u : 0u) << 16) | ((uint32_t)(tn >> 3) << 17);
                 uint32_t accumulate = 0u;
                 for (int i = 0; i < count; ++i) {
                     const uint32_t fb = bar0 + 8u * st;
@@ -284,9 +286,9 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                     break;
                 }
                 tc_fence_after();
-                if (GRAD && mode == DW) stages_of(Yes(), Yes(), u.rb1 - u.rb0);
-                else if (GRAD && mode == DH) stages_of(No(), Yes(), u.rb1 - u.rb0);
-                else stages_of(No(), No(), u.rb1 - u.rb0);
+                if (GRAD && mode == DW) stages_of(Yes(), Yes(), 256, u.rb1 - u.rb0);
+                else if (GRAD && mode == DH) stages_of(No(), Yes(), 256, u.rb1 - u.rb0);
+                else stages_of(No(), No(), P.job[u.j].tn, u.rb1 - u.rb0);
                 if (!failed) {
                     if (PAIR) tc_commit_pair(tfull0 + 8u * buf);
                     else tc_commit(tfull0 + 8u * buf);
@@ -296,7 +298,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             }
         }
     } else {
-        // ------------------------------------------------------------ epilogue warps: 32 rows x 128 columns each
+        // ------------------------------------------------------------ epilogue warps: 32 rows x half of the tile's columns each
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t wbuf = smem_base + (uint32_t)kStagesMax * 2u * kBlockBytes + (uint32_t)((warp - 2) * kOutWarpBytes);
         const float unscale = GRAD ? P.scale[1] : 1.0f;
@@ -327,7 +329,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             const int I = P.job[u.j].I, J = P.job[u.j].J;
             const CUtensorMap *map_o = &maps.o[u.j];
             const int row0 = u.ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
-            const int col0 = u.tj * 256 + half * 128;
+            const int wcols = P.job[u.j].tn / 2;         // columns of this warp
+            const int col0 = u.tj * 2 * wcols + half * wcols;
             const int row = row0 + lane;
             // what the epilogue needs of its row, fetched while the products run
             int label = -1;                              // column of the row's label in this tile's matrix, or outside it
@@ -348,14 +351,14 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                 break;
             }
             tc_fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * 256u + (uint32_t)(half * 128);
+            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * 256u + (uint32_t)(half * wcols);
             const bool live = row0 < I && col0 < J;          // uniform over the warp
             if (live) {
                 if (!GRAD) {
                     float m = -INFINITY, s = 0.0f, tgt = 0.0f;
                     bool hit = false;
 #pragma unroll 1
-                    for (int ch = 0; ch < 4; ++ch) {
+                    for (int ch = 0; ch < wcols / 32; ++ch) {
                         const int c0 = col0 + ch * 32;
                         if (c0 >= J) break;
                         uint32_t v[32];
@@ -396,7 +399,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                     }
                 } else if (mode == DLOGIT) {
 #pragma unroll 1
-                    for (int ch = 0; ch < 2; ++ch) {
+                    for (int ch = 0; ch < wcols / 64; ++ch) {
                         const int c0 = col0 + ch * 64;
                         if (c0 >= J) break;
                         uint32_t w[32];
@@ -613,6 +616,8 @@ inline int tiles256(long long n) { return (int)((n + 255) / 256); }
 // block and the scale.
 struct LossPlan {
     int parts;              // partial statistics per row
+    bool stats_pair;        // STATS: CTA pairs on 256 rows, or single CTAs on 128
+    int stats_tn, dlogit_tn;
     int pieces, Vp;         // vocabulary pieces of the backward pass and their width (a multiple of 256)
     int splits;             // parts of the vocabulary piece that dH's product is cut into
     size_t off_target;      // forward
@@ -630,10 +635,27 @@ constexpr int kPlanSlots = 74;                         // B200: planned for this
 LossPlan make_plan(int T, int V, int D)
 {
     LossPlan p;
-    p.parts = T <= kFewRowsLoss ? loss_rows_parts(V) : (int)(((long long)V + 127) / 128);
+    // Forward: pairs where their tiles fill half of the device, otherwise single CTAs.  Narrower tiles where there are few: a
+    // stage of a CTA that reads W mostly for itself takes as long as its bytes (450, 300, 250 ns for 256, 128, 64 columns;
+    // 16 x 3027 x 1958: 21 us in 12 tiles of 256, %STATS%).
+    const long long ti = tiles256(T), words = tiles256(V);
+    p.stats_pair = T > 128 && ti * words >= kPlanSlots / 2;
+    p.stats_tn = 256;
+    if (!p.stats_pair) {
+        long long best = -1;
+        for (int tn = 256; tn >= 64; tn /= 2) {
+            const long long tiles = (((long long)T + 127) / 128) * (((long long)V + tn - 1) / tn);
+            const long long ns = (tiles + 2 * kPlanSlots - 1) / (2 * kPlanSlots) * (tn == 256 ? 450 : (tn == 128 ? 300 : 250));
+            if (best < 0 || ns < best) {
+                best = ns;
+                p.stats_tn = tn;
+            }
+        }
+    }
+    p.dlogit_tn = ti * words * 2 <= kPlanSlots ? 128 : 256;
+    p.parts = T <= kFewRowsLoss ? loss_rows_parts(V) : (int)(((long long)V + p.stats_tn / 2 - 1) / (p.stats_tn / 2));
     p.off_target = kOffData + up256((size_t)T * (size_t)p.parts * sizeof(float2));
     p.fwd_bytes = p.off_target + up256((size_t)T * sizeof(float));
-    const long long words = tiles256(V);                // in units of 256
     long long most = kPieceBytes / (512ll * (T > 0 ? T : 1));
     if (most < 8) most = 8;
     p.pieces = (int)((words + most - 1) / most);
@@ -642,7 +664,7 @@ LossPlan make_plan(int T, int V, int D)
     p.acc_ld = (long long)tiles256(D) * 256;
     p.acc_rows = tiles256(T) * 256;
     // dH has few tiles, each as long as the piece: cut so that a part is at most half of a slot's share of the launch
-    const long long ti = tiles256(T), td = tiles256(D), wp = p.Vp / 256;
+    const long long td = tiles256(D), wp = p.Vp / 256;
     const long long len_h = p.Vp / kBK, len_w = (T + kBK - 1) / kBK;
     const long long share = (ti * td * len_h + wp * td * len_w) / kPlanSlots + 1;
     long long s = (2 * len_h + share - 1) / share;
@@ -704,7 +726,7 @@ void spread_units(LossParams &P)
 }
 
 // Adds a product to a launch.  Operands whose rows are the reduced dimension (MN-major) are stored [R][I] / [R][J].
-bool add_job(LossParams &P, LossMaps &maps, int type, bool pair, int mode, int I, int J, int R, int splits, const void *A, long long lda,
+bool add_job(LossParams &P, LossMaps &maps, int type, bool pair, int mode, int tn, int I, int J, int R, int splits, const void *A, long long lda,
              const void *B, long long ldb)
 {
     LossJob &job = P.job[P.jobs];
@@ -713,7 +735,8 @@ bool add_job(LossParams &P, LossMaps &maps, int type, bool pair, int mode, int I
     job.J = J;
     job.R = R;
     job.tiles_i = pair ? tiles256(I) : (int)(((long long)I + 127) / 128);
-    job.tiles_j = tiles256(J);
+    job.tn = tn;
+    job.tiles_j = (int)(((long long)J + tn - 1) / tn);
     job.splits = splits;
     const CUtensorMapDataType dt = type == CDL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     const bool a_mn = mode == DW, b_mn = mode == DW || mode == DH;
@@ -721,7 +744,7 @@ bool add_job(LossParams &P, LossMaps &maps, int type, bool pair, int mode, int I
     return (a_mn ? encode_map_2d(&maps.a[k], dt, 2, A, (uint64_t)I, (uint64_t)R, (uint64_t)lda * 2, 64)
                  : encode_map_2d(&maps.a[k], dt, 2, A, (uint64_t)R, (uint64_t)I, (uint64_t)lda * 2, 128)) &&
            (b_mn ? encode_map_2d(&maps.b[k], dt, 2, B, (uint64_t)J, (uint64_t)R, (uint64_t)ldb * 2, 64)
-                 : encode_map_2d(&maps.b[k], dt, 2, B, (uint64_t)R, (uint64_t)J, (uint64_t)ldb * 2, pair ? 128 : 256));
+                 : encode_map_2d(&maps.b[k], dt, 2, B, (uint64_t)R, (uint64_t)J, (uint64_t)ldb * 2, (uint32_t)(pair ? tn / 2 : tn)));
 }
 bool set_output(LossMaps &maps, int k, int type, const void *out, uint64_t cols, uint64_t rows, long long ld)
 {
@@ -842,8 +865,8 @@ extern "C" int cdl_vocab_loss_fwd(const void *H, int64_t ldh, const void *W, int
     P.parts = p.parts;
     P.target = reinterpret_cast<float *>(base + p.off_target);
     P.status = static_cast<int *>(ws);
-    const bool pair = T > 128;
-    if (!add_job(P, maps, type, pair, STATS, T, V, D, 1, H, ldh, W, ldw)) return CDL_ERR_LAUNCH;
+    const bool pair = p.stats_pair;
+    if (!add_job(P, maps, type, pair, STATS, p.stats_tn, T, V, D, 1, H, ldh, W, ldw)) return CDL_ERR_LAUNCH;
     if ((rc = launch_jobs(pair, false, type, maps, P, st)) != CDL_OK) return rc;
     return launch_join(P.part, p.parts, P.target, P.labels, T, V, loss, lse, st);
 }
@@ -906,7 +929,7 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
                 const bool direct = P.last && p.splits == 1;
                 P.out_h = dH;
                 P.ldh = lddh;
-                ok = ok && add_job(P, maps, type, true, DH, T, D, words, p.splits, dl, p.Vp, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
+                ok = ok && add_job(P, maps, type, true, DH, 256, T, D, words, p.splits, dl, p.Vp, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
                 ok = ok && (direct ? set_output(maps, P.jobs - 1, type, dH, (uint64_t)D, (uint64_t)T, lddh)
                                    : set_output(maps, P.jobs - 1, CDL_F32, acc, (uint64_t)p.acc_ld, (uint64_t)p.splits * (uint64_t)p.acc_rows, p.acc_ld));
             }
@@ -914,14 +937,14 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
                 char *out = static_cast<char *>(dW) + (size_t)v0 * (size_t)lddw * 2;
                 P.out_w = out;
                 P.ldw = lddw;
-                ok = ok && add_job(P, maps, type, true, DW, words, D, T, 1, dl, p.Vp, H, ldh);
+                ok = ok && add_job(P, maps, type, true, DW, 256, words, D, T, 1, dl, p.Vp, H, ldh);
                 ok = ok && set_output(maps, P.jobs - 1, type, out, (uint64_t)D, (uint64_t)words, lddw);
             }
         }
         if (k + 1 < p.pieces) {
             const int v0 = (k + 1) * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
             P.v0 = v0;
-            ok = ok && add_job(P, maps, type, true, DLOGIT, T, words, D, 1, H, ldh, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
+            ok = ok && add_job(P, maps, type, true, DLOGIT, p.dlogit_tn, T, words, D, 1, H, ldh, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
             ok = ok && set_output(maps, P.jobs - 1, type, base + kOffData + (size_t)((k + 1) & 1) * p.dl_bytes, (uint64_t)words, (uint64_t)T, p.Vp);
         }
         if (!ok) return CDL_ERR_LAUNCH;
