@@ -42,7 +42,7 @@ constexpr int kOutWarpBytes = 32 * 128;
 constexpr int kStagesMax = 6;
 constexpr int kSmemBytes = 1024 + kStagesMax * 2 * kBlockBytes + kEpiWarps * kOutWarpBytes;
 constexpr unsigned long long kWaitNs = 2000000000ull;
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kStatusBytes = 256;
 
 constexpr int kMaxSlots = 80;                          // CTA pairs of a launch (74 on a B200)
@@ -67,7 +67,7 @@ struct LossParams {
     const long long *labels;        // STATS, DLOGIT
     int V;                          // words of the vocabulary
     int v0;                         // DLOGIT: first word of the piece
-    float2 *part;                   // STATS: (maximum, sum) per row and half tile
+    float2 *part;                   // STATS: (maximum in units of log 2, sum of exponentials relative to it) per row and half tile
     int parts;                      // ... entries per row
     float *target;                  // STATS: the label's logit
     const float *lse, *dloss;       // DLOGIT
@@ -340,9 +340,11 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                 const long long c = y - (GRAD ? P.v0 : 0);
                 label = c >= 0 && y < P.V ? (int)c : -1;
                 if (GRAD) {
-                    lse2 = P.lse[row] * kLog2e;
+                    // (exponentials are taken times 2^24, which dloss gives back: a probability below the smallest normal number
+                    // is not flushed to 0)
+                    lse2 = fmaf(P.lse[row], kLog2e, -24.0f);
                     // (a label outside the vocabulary: no gradient)
-                    g = y >= 0 && y < P.V ? P.dloss[row] * P.scale[0] : 0.0f;
+                    g = y >= 0 && y < P.V ? P.dloss[row] * P.scale[0] * 5.9604644775390625e-8f : 0.0f;
                     if (!(y >= 0 && y < P.V)) label = -2;
                 }
             }
@@ -355,7 +357,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             const bool live = row0 < I && col0 < J;          // uniform over the warp
             if (live) {
                 if (!GRAD) {
-                    float m = -INFINITY, s = 0.0f, tgt = 0.0f;
+                    float m = -INFINITY, s = 0.0f, tgt = 0.0f;         // running maximum, in units of log 2
                     bool hit = false;
 #pragma unroll 1
                     for (int ch = 0; ch < wcols / 32; ++ch) {
@@ -380,8 +382,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                         float cm = __uint_as_float(v[0]);
 #pragma unroll
                         for (int c = 1; c < 32; ++c) cm = fmaxf(cm, __uint_as_float(v[c]));
-                        const float mn = fmaxf(m, cm);
-                        const float base = mn == -INFINITY ? 0.0f : mn * kLog2e;     // (all logits -infinity: exponentials are 0)
+                        const float mn = fmaxf(m, cm * kLog2e);
+                        const float base = mn == -INFINITY ? 0.0f : mn;     // (all logits -infinity: exponentials are 0)
                         float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
 #pragma unroll
                         for (int c = 0; c < 32; c += 4) {
@@ -390,7 +392,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                             s2 += exp2_fast(fmaf(__uint_as_float(v[c + 2]), kLog2e, -base));
                             s3 += exp2_fast(fmaf(__uint_as_float(v[c + 3]), kLog2e, -base));
                         }
-                        s = s * (m == -INFINITY ? 0.0f : exp2_fast(fmaf(m, kLog2e, -base))) + ((s0 + s1) + (s2 + s3));
+                        s = s * (m == -INFINITY ? 0.0f : exp2_fast(m - base)) + ((s0 + s1) + (s2 + s3));
                         m = mn;
                     }
                     if (row < I) {
@@ -414,7 +416,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                             if (__any_sync(0xffffffffu, (unsigned)(label - (c0 + 32 * h)) < 32u)) {
 #pragma unroll
                                 for (int c = 0; c < 32; ++c)
-                                    if (label == c0 + 32 * h + c) v[c] = __float_as_uint(__uint_as_float(v[c]) - 1.0f);
+                                    if (label == c0 + 32 * h + c) v[c] = __float_as_uint(__uint_as_float(v[c]) - 16777216.0f);
                             }
 #pragma unroll
                             for (int c = 0; c < 16; ++c) {
@@ -516,7 +518,7 @@ loss_join_kernel(const float2 *part, int parts, const float *target, const long 
     float m = -INFINITY, s = 0.0f;
     auto join = [&](float m2, float s2) {
         const float mn = fmaxf(m, m2);
-        if (mn != -INFINITY) s = s * exp2_fast((m - mn) * kLog2e) + s2 * exp2_fast((m2 - mn) * kLog2e);
+        if (mn != -INFINITY) s = s * exp2_fast(m - mn) + s2 * exp2_fast(m2 - mn);
         else s += s2;                                // (no maximum: 0, or NaN where a logit is NaN)
         m = mn;
     };
@@ -531,7 +533,7 @@ loss_join_kernel(const float2 *part, int parts, const float *target, const long 
     if (threadIdx.x == 0) {
 #pragma unroll
         for (int k = 1; k < 4; ++k) join(sh[k].x, sh[k].y);
-        const float l = m + logf(s);
+        const float l = fmaf(m, kLn2, logf(s));
         const long long y = labels[row];
         lse[row] = l;
         loss[row] = y >= 0 && y < V ? l - target[row] : 0.0f;
@@ -572,23 +574,27 @@ loss_scale_kernel(const float *dloss, const long long *labels, int T, int V, flo
 
 // dH from the binary32 sums of the splits, added in their order
 template <typename T>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(128)
 loss_sum_kernel(const float *acc, long long acc_ld, long long split_elems, int splits, int rows, int cols, const float *scale, T *out, long long ldo)
 {
     follow_previous();
     const float unscale = scale[1];
     const int per_row = (cols + 7) / 8;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < (long long)rows * per_row; i += (long long)gridDim.x * 256) {
+    for (long long i = (long long)blockIdx.x * 128 + threadIdx.x; i < (long long)rows * per_row; i += (long long)gridDim.x * 128) {
         const long long r = i / per_row;
         const int c = (int)(i - r * per_row) * 8;
         const float *p = acc + r * acc_ld + c;
-        float v[8];
-        load8(p, v);
-        for (int s = 1; s < splits; ++s) {
-            float w[8];
-            load8(p + s * split_elems, w);
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s0 = 0; s0 < splits; s0 += 4) {         // four splits' loads at a time: with few rows this kernel is their latency
+            float w[4][8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += w[k];
+            for (int s = 0; s < 4; ++s)
+                if (s0 + s < splits) load8(p + (s0 + s) * split_elems, w[s]);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                if (s0 + s < splits)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] += w[s][k];
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= unscale;
@@ -637,7 +643,7 @@ LossPlan make_plan(int T, int V, int D)
     LossPlan p;
     // Forward: pairs where their tiles fill half of the device, otherwise single CTAs.  Narrower tiles where there are few: a
     // stage of a CTA that reads W mostly for itself takes as long as its bytes (450, 300, 250 ns for 256, 128, 64 columns;
-    // 16 x 3027 x 1958: 21 us in 12 tiles of 256, %STATS%).
+    // 16 x 3027 x 1958: 20.9 us in 12 tiles of 256, 14.7 in 48 of 64).
     const long long ti = tiles256(T), words = tiles256(V);
     p.stats_pair = T > 128 && ti * words >= kPlanSlots / 2;
     p.stats_tn = 256;
@@ -952,12 +958,12 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
     }
     if (dH != nullptr && p.splits > 1) {
         const long long units = (long long)T * ((D + 7) / 8);
-        const int blocks = (int)(units / 256 + 1 < 4096 ? units / 256 + 1 : 4096);
+        const int blocks = (int)(units / 128 + 1 < 4096 ? units / 128 + 1 : 4096);
         const long long step = (long long)p.acc_rows * p.acc_ld;
         if (type == CDL_BF16)
-            return launch_following(&loss_sum_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(256), 0, st, (const float *)acc, p.acc_ld, step, p.splits,
+            return launch_following(&loss_sum_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(128), 0, st, (const float *)acc, p.acc_ld, step, p.splits,
                                     (int)T, (int)D, (const float *)scale, static_cast<__nv_bfloat16 *>(dH), (long long)lddh);
-        return launch_following(&loss_sum_kernel<__half>, dim3((unsigned)blocks), dim3(256), 0, st, (const float *)acc, p.acc_ld, step, p.splits, (int)T, (int)D,
+        return launch_following(&loss_sum_kernel<__half>, dim3((unsigned)blocks), dim3(128), 0, st, (const float *)acc, p.acc_ld, step, p.splits, (int)T, (int)D,
                                 (const float *)scale, static_cast<__half *>(dH), (long long)lddh);
     }
     return CDL_OK;

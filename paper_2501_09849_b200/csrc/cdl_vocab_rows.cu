@@ -33,7 +33,7 @@ __device__ __forceinline__ float exp2_fast(float x)
 __device__ __forceinline__ void join(float &m, float &s, float m2, float s2)
 {
     const float mn = fmaxf(m, m2);
-    if (mn != -INFINITY) s = s * exp2_fast((m - mn) * kLog2e) + s2 * exp2_fast((m2 - mn) * kLog2e);
+    if (mn != -INFINITY) s = s * exp2_fast(m - mn) + s2 * exp2_fast(m2 - mn);
     else s += s2;
     m = mn;
 }
@@ -135,14 +135,14 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
                 if (lane == 0 && t < rows && label[t] == v0 + w && v0 + w < V) target[t] = acc[t][w];
                 if (v0 + w >= V) acc[t][w] = -INFINITY;
             }
-            float mn = m[t];
+            float mn = m[t];                             // (in units of log 2)
 #pragma unroll
-            for (int w = 0; w < kWords; ++w) mn = fmaxf(mn, acc[t][w]);
-            const float base = mn == -INFINITY ? 0.0f : mn * kLog2e;
+            for (int w = 0; w < kWords; ++w) mn = fmaxf(mn, acc[t][w] * kLog2e);
+            const float base = mn == -INFINITY ? 0.0f : mn;
             float sum = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWords; ++w) sum += exp2_fast(fmaf(acc[t][w], kLog2e, -base));
-            s[t] = s[t] * (m[t] == -INFINITY ? 0.0f : exp2_fast(fmaf(m[t], kLog2e, -base))) + sum;
+            s[t] = s[t] * (m[t] == -INFINITY ? 0.0f : exp2_fast(m[t] - base)) + sum;
             m[t] = mn;
         }
     }

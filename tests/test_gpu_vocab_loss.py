@@ -142,6 +142,29 @@ def test_large_logits_and_tiny_gradients(kind):
     check(torch, run(torch, h, w, y, gl, T, V, D, kind), h, w, y, gl, T, V, D, kind)
 
 
+@pytest.mark.parametrize("T", [1, 2, 7, 150])
+def test_rows_that_outgrow_their_first_columns(T):
+    """Logits that rise by hundreds along the vocabulary, fall, or begin at -infinity: the base of a row's sums has to follow."""
+    import torch
+    V, D = 1200, 64
+    h, w, y, gl = problem(torch, T, V, D, "bf16", 12, ignore=0.0)
+    h[:, :D] = 0
+    w[:, :D] = 0
+    h[:, 0] = 1.0
+    h[:, 1] = torch.where(torch.arange(T, device="cuda") % 2 == 0, 1.0, -1.0).to(h.dtype)
+    w[:, 1] = torch.linspace(-300, 300, V, device="cuda").to(w.dtype)
+    w[:, 0] = torch.randn(V, generator=torch.Generator().manual_seed(2)).to(w.dtype).cuda()
+    w[700:, 1] = 0.0
+    check(torch, run(torch, h, w, y, gl, T, V, D, "bf16"), h, w, y, gl, T, V, D, "bf16")
+    w[:500, 1] = float("-inf")                            # even rows: the first words cannot be; odd rows: +infinity
+    y = torch.full_like(y, 900)
+    loss, lse, _, _ = run(torch, h, w, y, gl, T, V, D, "bf16", need=("dh",))
+    logits = h[::2, :D].double() @ w[:, :D].double().nan_to_num(neginf=-1e300).t()
+    ref = torch.logsumexp(logits, 1)
+    assert bool(((lse[::2].double() - ref).abs() <= 2.0 ** -18 * ref.abs()).all())
+    assert bool((torch.isnan(lse[1::2]) | torch.isinf(lse[1::2])).all())
+
+
 def test_non_finite_rows_stay_in_their_rows():
     import torch
     T, V, D = 130, 400, 64
