@@ -388,7 +388,8 @@ int cdl_workspace_status(void *ws, void *stream);
 /*
  * ---------------------------------------------------------------------------------------------------------------
  * Operators of language models (no counterpart in the paper): dropout, block-scaled 8-bit floating-point products with
- * their quantizer, and the cross entropy over a large vocabulary.  The conventions at the top of this file hold.
+ * their quantizer, and the cross entropy over a large vocabulary.  The conventions at the top of this file hold; rows,
+ * columns and reduced extents given as int32_t are at most 2^30 (CDL_ERR_ARG).
  * Element types of their tensors:
  */
 #define CDL_F32 0  /* IEEE binary32 */

@@ -48,7 +48,6 @@ __host__ __device__ constexpr int smem_bytes(bool bvec)
     return 1024 + stages(bvec) * kStageBytes + kEpiWarps * kOutWarpBytes + kScaleSlots * kGroup * slot_floats(bvec) * 4;
 }
 constexpr unsigned long long kWaitNs = 2000000000ull;
-constexpr int kMaxSplits = 8;                          // portable cluster size
 
 struct Fp8Params {
     int M, N, KB;                   // KB: blocks of 128 along the reduced dimension
@@ -609,7 +608,7 @@ bool make_plan(int32_t M, int32_t N, int32_t K, Fp8Plan *p)
 extern "C" size_t cdl_fp8_matmul_workspace_bytes(int32_t M, int32_t N, int32_t K)
 {
     Fp8Plan p;
-    if (M < 0 || N < 0 || K < 0) return 0;
+    if (M < 0 || N < 0 || K < 0 || M > cdl::kMostExtent || N > cdl::kMostExtent || K > cdl::kMostExtent) return 0;
     return make_plan(M, N, K, &p) ? kStatusBytes + p.part_bytes : kStatusBytes;      // the status block, the parts of cut tiles
 }
 
@@ -618,7 +617,7 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
                               const float *bias, void *ws, size_t ws_bytes, void *stream)
 {
     using namespace cdl;
-    if (M < 0 || N < 0 || K < 0 || !valid_type(out_type) || (b_mode != CDL_FP8_ROWS && b_mode != CDL_FP8_BLOCKS)) return CDL_ERR_ARG;
+    if (M < 0 || N < 0 || K < 0 || M > kMostExtent || N > kMostExtent || K > kMostExtent || !valid_type(out_type) || (b_mode != CDL_FP8_ROWS && b_mode != CDL_FP8_BLOCKS)) return CDL_ERR_ARG;
     if (M == 0 || N == 0) return CDL_OK;
     if (out == nullptr || ldo < N) return CDL_ERR_ARG;
     if (K > 0 && (A == nullptr || B == nullptr || a_scale == nullptr || b_scale == nullptr || lda < K || ldb < K)) return CDL_ERR_ARG;

@@ -300,7 +300,7 @@ extern "C" int cdl_fp8_quantize(const void *x, int64_t ldx, int32_t type, int32_
                                 int64_t ldc, float *scales, void *codes_t, int64_t ldt, float *scales_t, void *stream)
 {
     using namespace cdl;
-    if (rows < 0 || cols < 0 || !valid_type(type) || (mode != CDL_FP8_ROWS && mode != CDL_FP8_BLOCKS)) return CDL_ERR_ARG;
+    if (rows < 0 || cols < 0 || rows > kMostExtent || cols > kMostExtent || !valid_type(type) || (mode != CDL_FP8_ROWS && mode != CDL_FP8_BLOCKS)) return CDL_ERR_ARG;
     if (rows == 0 || cols == 0) return CDL_OK;
     if (x == nullptr || codes == nullptr || scales == nullptr || (codes_t == nullptr) != (scales_t == nullptr)) return CDL_ERR_ARG;
     if ((rows > 1 && ldx < cols) || ldc < cols || (codes_t != nullptr && ldt < rows)) return CDL_ERR_ARG;

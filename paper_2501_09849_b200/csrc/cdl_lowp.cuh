@@ -10,6 +10,8 @@
 namespace cdl {
 
 inline bool valid_type(int type) { return type == CDL_F32 || type == CDL_BF16 || type == CDL_F16; }
+// Most rows, columns or reduced entries of an operand: tile corners and stage coordinates are 32-bit numbers.
+constexpr int kMostExtent = 1 << 30;
 inline int type_bytes(int type) { return type == CDL_F32 ? 4 : 2; }
 inline bool misaligned(const void *p, int type) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(type_bytes(type) - 1)) != 0; }
 

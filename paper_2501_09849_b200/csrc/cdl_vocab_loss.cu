@@ -668,14 +668,15 @@ LossPlan make_plan(int T, int V, int D)
     p.Vp = (int)((words + p.pieces - 1) / p.pieces) * 256;
     p.pieces = (int)((V + (long long)p.Vp - 1) / p.Vp);
     p.acc_ld = (long long)tiles256(D) * 256;
-    p.acc_rows = tiles256(T) * 256;
+    p.acc_rows = tiles256(T > 0 ? T : 1) * 256;
     // dH has few tiles, each as long as the piece: cut so that a part is at most half of a slot's share of the launch
     const long long td = tiles256(D), wp = p.Vp / 256;
     const long long len_h = p.Vp / kBK, len_w = (T + kBK - 1) / kBK;
     const long long share = (ti * td * len_h + wp * td * len_w) / kPlanSlots + 1;
     long long s = (2 * len_h + share - 1) / share;
     if (s > len_h / 8) s = len_h / 8;
-    if (s > kAccBytes / (4 * p.acc_rows * p.acc_ld + 1)) s = kAccBytes / (4 * p.acc_rows * p.acc_ld + 1);
+    const long long acc_bytes = 4ll * p.acc_rows * p.acc_ld;
+    if (s > kAccBytes / acc_bytes) s = kAccBytes / acc_bytes;
     if (s > 16) s = 16;
     p.splits = s > 1 ? (int)s : 1;
     p.dl_bytes = up256((size_t)T * (size_t)p.Vp * 2);
@@ -820,7 +821,7 @@ int launch_join(const float2 *part, int parts, const float *target, const long l
 
 int check_common(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels, int32_t T, int32_t V, int32_t D)
 {
-    if (T < 0 || V < 1 || D < 1 || (type != CDL_BF16 && type != CDL_F16)) return CDL_ERR_ARG;
+    if (T < 0 || V < 1 || D < 1 || T > kMostExtent || V > kMostExtent || D > kMostExtent || (type != CDL_BF16 && type != CDL_F16)) return CDL_ERR_ARG;
     if (W == nullptr || ldw < D) return CDL_ERR_ARG;
     if (T > 0 && (H == nullptr || labels == nullptr || ldh < D)) return CDL_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(H) & 15u) || (reinterpret_cast<uintptr_t>(W) & 15u) || (ldw & 7) || (T > 0 && (ldh & 7)) ||
@@ -835,7 +836,7 @@ int check_common(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t
 extern "C" size_t cdl_vocab_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t with_gradient)
 {
     using namespace cdl;
-    if (T < 0 || V < 1 || D < 1) return 0;
+    if (T < 0 || V < 1 || D < 1 || T > kMostExtent || V > kMostExtent || D > kMostExtent) return 0;
     const LossPlan p = make_plan(T, V, D);
     return with_gradient && p.bwd_bytes > p.fwd_bytes ? p.bwd_bytes : p.fwd_bytes;
 }

@@ -37,6 +37,7 @@ def test_fp8_quantize_refusals():
     assert f(x=P + 1) == ALIGN and f(x=P + 2, type=cdl.CDL_F32) == ALIGN and f(codes=P + 8) == ALIGN and f(ldc=104) == ALIGN and f(s=P + 2) == ALIGN
     assert f(ct=P + 8, st=P, ldt=32) == ALIGN and f(ct=P, st=P, ldt=40) == ALIGN and f(ct=P, st=P + 1, ldt=32) == ALIGN
     assert f(rows=2 ** 31 - 1, cols=2 ** 31 - 1, ldx=2 ** 31, ldc=2 ** 31) == ARG          # more tiles than a launch has blocks
+    assert f(cols=2 ** 30 + 1, ldx=2 ** 31, ldc=2 ** 31) == ARG
     assert f(rows=0) == 0 and f(cols=0) == 0
 
 
@@ -52,6 +53,7 @@ def test_fp8_matmul_refusals():
     assert f(A=P + 8) == ALIGN and f(B=P + 8) == ALIGN and f(lda=204) == ALIGN and f(ldb=204) == ALIGN and f(out=P + 1) == ALIGN
     assert f(sa=P + 2) == ALIGN and f(sb=P + 2) == ALIGN and f(bias=P + 2) == ALIGN and f(out=P + 2, type=cdl.CDL_F32) == ALIGN
     assert f(ws=None) == WS and f(ws=P + 16) == WS and f(nb=n - 1) == WS
+    assert f(K=2 ** 30 + 1, lda=2 ** 31, ldb=2 ** 31) == ARG and cdl.cdl_fp8_matmul_workspace_bytes(1, 2 ** 30 + 1, 1) == 0
     assert f(M=0) == 0 and f(N=0) == 0
 
 
@@ -68,6 +70,7 @@ def test_vocab_loss_refusals():
     for call in (f, b):
         assert call(H=None) == ARG and call(W=None) == ARG and call(y=None) == ARG and call(lse=None) == ARG
         assert call(type=cdl.CDL_F32) == ARG and call(type=9) == ARG
+        assert call(V=2 ** 30 + 1) == ARG
         assert call(T=-1) == ARG and call(V=0) == ARG and call(D=0) == ARG and call(ldh=64) == ARG and call(ldw=64) == ARG
         assert call(H=P + 8) == ALIGN and call(W=P + 8) == ALIGN and call(ldh=76) == ALIGN and call(ldw=76) == ALIGN and call(y=P + 4) == ALIGN
         assert call(lse=P + 2) == ALIGN
