@@ -6,14 +6,20 @@
 // The scales change with every stage, so an accumulator cannot stay in TMEM over the whole reduction: each stage's partial
 // tile goes into the next of the TMEM buffers, the epilogue warps read it back while the following stages' products run,
 // and add it, scaled, to the tile they keep in registers (one fused multiply-add per entry and stage; one more product
-// where B's scales change from column to column).  For a 256 x 256 tile of a CTA pair a stage is 512 tensor-core cycles
-// per SM, against 256 cycles of TMEM reads and 256 (or 512) of binary32 arithmetic for the 128 x 256 entries of a CTA.
+// where B's scales change from column to column).  What bounds it is this hand-over.  For a 256 x 256 tile of a CTA pair the
+// tensor cores alone take 750 cycles a stage (with the accumulator left in TMEM), TMEM read-back and additions 320 (580 with
+// column scales: two packed instructions per two entries, two cycles each); with two buffers a stage comes to 930 (1306):
+// a partial tile is complete 800 cycles after its products are issued, drained 400 (750) later, and its buffer's release
+// reaches the issuing thread another 200 later.  8192 x 8192 x 4096: 267 us, 2060 TFLOP/s; 317 under the power cap.
 //
-// Tiles: 256 x 256 per CTA pair (cta_group::2, as in the index products), or 128 x 128 per CTA where the pair tiles would
-// leave SMs idle.  With few tiles (one token, a short prompt) the reduced dimension is also cut over the CTAs of a
-// cluster, whose partial tiles are added in a fixed order through distributed shared memory: no scratch in global
-// memory, no atomics, one launch.  Rows beyond M are zero-filled by TMA and cost no memory traffic.
-// Warp roles: warp 0 issues TMA, warp 1 owns TMEM and issues the MMAs, warps 4..11 are the epilogue.  Every wait is bounded.
+// Tiles: 256 x 256 per CTA pair (cta_group::2, as in the index products), or 128 x 128 per CTA where that is estimated to be
+// faster (make_plan).  With few tiles (a short prompt) the reduced dimension is also cut over the CTAs of a cluster, whose
+// partial tiles are added in a fixed order through distributed shared memory: no scratch in global memory, no atomics, one
+// launch.  In pairs the tiles of a last, partly filled round are cut into parts that go through the workspace.  Rows beyond
+// M are zero-filled by TMA and cost no memory traffic.
+// Warp roles: warp 0 issues TMA, warp 1 owns TMEM and issues the MMAs, warp 2 fetches scales (four stages at a time, with
+// asynchronous 4-byte copies: handed over stage by stage they cost another barrier per stage, 1062 cycles instead of 930),
+// warps 4..11 are the epilogue.  Every wait is bounded.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <string.h>

@@ -13,8 +13,14 @@
 // writes it and the two that read it.
 //
 // Tiles: 256 x 256 per CTA pair (cta_group::2), 64 reduced entries (128 bytes) per stage, six stages; two accumulators
-// in TMEM let the epilogue of a tile run beside the products of the next.  With at most 128 rows (scoring, decoding) a CTA
-// takes 128 x 256 by itself: rows beyond T are zero-filled by TMA, and the launch is bound by reading W once.
+// in TMEM let the epilogue of a tile run beside the products of the next.  Where pairs would leave half of the device idle
+// (few rows, a small vocabulary) the statistics take 128-row tiles of one CTA, narrower ones if need be.  The backward pass
+// mixes the products that read one piece's dl with the product that writes the next one's in one launch, whose units are
+// spread over the pairs by their lengths: one ragged end per piece instead of three (4096 x 50176 x 2048: 2.85 -> 2.28 ms
+// together with a stage loop of its own for each kind of operands).
+// What bounds it: the tensor cores, 520 cycles a stage of 512 forward (92.5 % of their cycles, 1.66 PFLOP/s) and 608 backward
+// (86 %); below about 400 reduced entries the exponentials of the epilogue, 3300 cycles a tile (a special-function unit
+// takes eight per instruction and scheduler: 2112).  Rows that do not start on 128 bytes cost 725 cycles a stage.
 // Every wait is bounded.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
