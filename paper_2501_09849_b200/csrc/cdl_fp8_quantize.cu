@@ -56,7 +56,8 @@ __device__ __forceinline__ void load_shifted(const void *p, uint32_t (&out)[4])
 {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
     const uint4 *q = reinterpret_cast<const uint4 *>(at & ~(uintptr_t)15);
-    const uint4 a = __ldcs(q), b = (at & 15) ? __ldcs(q + 1) : a;
+    const uint4 a = __ldcs(q);
+    const uint4 b = (at & 15) ? __ldcs(q + 1) : make_uint4(0u, 0u, 0u, 0u);
     uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
     for (int i = 0; i < 6; ++i) w[i] = (at & 8) ? w[i + 2] : w[i];
