@@ -51,7 +51,7 @@ constexpr unsigned long long kWaitNs = 2000000000ull;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kStatusBytes = 256;
 
-constexpr int kMaxSlots = 80;                          // CTA pairs of a launch (74 on a B200)
+constexpr int kMaxSlots = 160;                         // CTAs, or pairs of them, of a backward launch (148 or 74 on a B200)
 
 // One product of a launch: output I x J, reduced over R, cut into `splits` parts of the reduced dimension.
 struct LossJob {
@@ -209,8 +209,9 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             // dimension: a row pitch that is a power of two would have all CTAs read the same few memory channels at a time.
             auto stages_of = [&](auto a_mn, auto b_mn, const CUtensorMap *map_a, const CUtensorMap *map_b, int arow, int brow, uint32_t bytes,
                                  int r0, int r1) {
-                int r = PAIR ? r0 : brow / 64 * 5 % (r1 / kBK) * kBK;
-                for (int left = (r1 - r0) / kBK; left > 0; --left) {
+                const int count = (r1 - r0) / kBK;
+                int r = PAIR || count == 0 ? r0 : r0 + brow / 64 * 5 % count * kBK;
+                for (int left = count; left > 0; --left) {
                     const uint32_t fb = bar0 + 8u * st;
                     if (!mbar_try_wait_now(fb + kEmptyOff, par) && !mbar_wait(fb + kEmptyOff, par, abort_flag, kWaitNs)) {
                         failed = true;
@@ -227,7 +228,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                         for (int b = 0; b < kBRows / 64; ++b) load(sb + (uint32_t)b * 8192u, map_b, brow + b * 64, r, fb);
                     } else load(sb, map_b, r, brow, fb);
                     r += kBK;
-                    if (!PAIR && r == r1) r = 0;
+                    if (!PAIR && r == r1) r = r0;
                     if (++st == (uint32_t)kStages) {
                         st = 0u;
                         par ^= 1u;
@@ -616,7 +617,7 @@ loss_sum_kernel(const float *acc, long long acc_ld, long long split_elems, int s
 template <typename T>
 const void *variant(bool pair, bool grad)
 {
-    if (grad) return reinterpret_cast<const void *>(&loss_gemm_kernel<true, true, T>);
+    if (grad) return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, true, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, true, T>);
     return pair ? reinterpret_cast<const void *>(&loss_gemm_kernel<true, false, T>) : reinterpret_cast<const void *>(&loss_gemm_kernel<false, false, T>);
 }
 const void *variant(bool pair, bool grad, int type) { return type == CDL_BF16 ? variant<__nv_bfloat16>(pair, grad) : variant<__half>(pair, grad); }
@@ -631,6 +632,7 @@ struct LossPlan {
     bool stats_pair;        // STATS: CTA pairs on 256 rows, or single CTAs on 128
     int stats_tn, dlogit_tn;
     int pieces, Vp;         // vocabulary pieces of the backward pass and their width (a multiple of 256)
+    bool grad_pair;         // backward: CTA pairs on 256 rows, or single CTAs on 128 where H has no more
     int splits;             // parts of the vocabulary piece that dH's product is cut into
     size_t off_target;      // forward
     size_t dl_bytes;        // backward: dl of one piece (two of them when there are several pieces)
@@ -664,7 +666,12 @@ LossPlan make_plan(int T, int V, int D)
             }
         }
     }
-    p.dlogit_tn = ti * words * 2 <= kPlanSlots ? 128 : 256;
+// With at most 128 rows a pair's second CTA would have nothing of dl or dH to do (16 x 3027 x 1958: 36 us of backward pass in pairs,
+    // 28 in single CTAs; 64 x 5000 x 1500 40 and 32; 79 x 61013 x 182, all outputs and no reduction, 51 and 55).
+    p.grad_pair = T > 128;
+    const long long slots = p.grad_pair ? kPlanSlots : 2 * kPlanSlots, edge = p.grad_pair ? 256 : 128;
+    const long long gi = ((long long)T + edge - 1) / edge;
+    p.dlogit_tn = gi * words * 2 <= slots ? 128 : 256;
     p.parts = T <= kFewRowsLoss ? loss_rows_parts(V) : (int)(((long long)V + p.stats_tn / 2 - 1) / (p.stats_tn / 2));
     p.off_target = kOffData + up256((size_t)T * (size_t)p.parts * sizeof(float2));
     p.fwd_bytes = p.off_target + up256((size_t)T * sizeof(float));
@@ -676,9 +683,9 @@ LossPlan make_plan(int T, int V, int D)
     p.acc_ld = (long long)tiles256(D) * 256;
     p.acc_rows = tiles256(T > 0 ? T : 1) * 256;
     // dH has few tiles, each as long as the piece: cut so that a part is at most half of a slot's share of the launch
-    const long long td = tiles256(D), wp = p.Vp / 256;
+    const long long td = tiles256(D), wp = p.Vp / edge;
     const long long len_h = p.Vp / kBK, len_w = (T + kBK - 1) / kBK;
-    const long long share = (ti * td * len_h + wp * td * len_w) / kPlanSlots + 1;
+    const long long share = (gi * td * len_h + wp * td * len_w) / slots + 1;
     long long s = (2 * len_h + share - 1) / share;
     if (s > len_h / 8) s = len_h / 8;
     const long long acc_bytes = 4ll * p.acc_rows * p.acc_ld;
@@ -805,7 +812,7 @@ int launch_jobs(bool pair, bool grad, int type, LossMaps &maps, LossParams &P, c
     long long units = 0;
     for (int j = 0; j < P.jobs; ++j) units += (long long)P.job[j].tiles_i * P.job[j].tiles_j * P.job[j].splits;
     if (units > 0x3fffffff) return CDL_ERR_ARG;
-    const int most = pair ? pair_slots[dev] : sms;
+    const int most = pair ? pair_slots[dev] : (sms < kMaxSlots ? sms : kMaxSlots);
     P.slots = (int)(units < most ? units : most);
     if (grad) spread_units(P);
     cfg.gridDim = dim3((pair ? 2u : 1u) * (unsigned)P.slots);
@@ -942,7 +949,7 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
                 const bool direct = P.last && p.splits == 1;
                 P.out_h = dH;
                 P.ldh = lddh;
-                ok = ok && add_job(P, maps, type, true, DH, 256, T, D, words, p.splits, dl, p.Vp, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
+                ok = ok && add_job(P, maps, type, p.grad_pair, DH, 256, T, D, words, p.splits, dl, p.Vp, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
                 ok = ok && (direct ? set_output(maps, P.jobs - 1, type, dH, (uint64_t)D, (uint64_t)T, lddh)
                                    : set_output(maps, P.jobs - 1, CDL_F32, acc, (uint64_t)p.acc_ld, (uint64_t)p.splits * (uint64_t)p.acc_rows, p.acc_ld));
             }
@@ -950,18 +957,18 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
                 char *out = static_cast<char *>(dW) + (size_t)v0 * (size_t)lddw * 2;
                 P.out_w = out;
                 P.ldw = lddw;
-                ok = ok && add_job(P, maps, type, true, DW, 256, words, D, T, 1, dl, p.Vp, H, ldh);
+                ok = ok && add_job(P, maps, type, p.grad_pair, DW, 256, words, D, T, 1, dl, p.Vp, H, ldh);
                 ok = ok && set_output(maps, P.jobs - 1, type, out, (uint64_t)D, (uint64_t)words, lddw);
             }
         }
         if (k + 1 < p.pieces) {
             const int v0 = (k + 1) * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
             P.v0 = v0;
-            ok = ok && add_job(P, maps, type, true, DLOGIT, p.dlogit_tn, T, words, D, 1, H, ldh, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
+            ok = ok && add_job(P, maps, type, p.grad_pair, DLOGIT, p.dlogit_tn, T, words, D, 1, H, ldh, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
             ok = ok && set_output(maps, P.jobs - 1, type, base + kOffData + (size_t)((k + 1) & 1) * p.dl_bytes, (uint64_t)words, (uint64_t)T, p.Vp);
         }
         if (!ok) return CDL_ERR_LAUNCH;
-        if ((rc = launch_jobs(true, true, type, maps, P, st)) != CDL_OK) return rc;
+        if ((rc = launch_jobs(p.grad_pair, true, type, maps, P, st)) != CDL_OK) return rc;
     }
     if (dH != nullptr && p.splits > 1) {
         const long long units = (long long)T * ((D + 7) / 8);
