@@ -105,7 +105,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 {
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 8 + 2 * kScaleSlots];
-    __shared__ uint32_t tmem_base_s;
+    __shared__ uint32_t tmem_base_s, asked_s;
     __shared__ int abort_s;
 
     constexpr int kStages = stages(BVEC);
@@ -167,7 +167,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (warp == 0) {
             // ------------------------------------------------------------ TMA producer (one lane)
             if (lane == 0) {
-                uint32_t st = 0u, par = 1u;
+                uint32_t st = 0u, par = 1u, asked = 0u;
                 for (int u = slot; u < units && !failed; u += P.slots) {
                     int ti, tj, kb0, kb1;
                     unit_at(u, ti, tj, kb0, kb1);
@@ -188,12 +188,14 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                             tma_load_2d(sa, &map_a, kb * 128, arow, fb);
                             tma_load_2d(sb, &map_b, kb * 128, brow, fb);
                         }
+                        ++asked;
                         if (++st == (uint32_t)kStages) {
                             st = 0u;
                             par ^= 1u;
                         }
                     }
                 }
+                asked_s = asked;
             }
         } else if (warp == 1) {
             // ------------------------------------------------------------ MMA issuer (one lane; CTA 0 of a pair)
@@ -501,6 +503,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 
     tc_fence_before();
     __syncthreads();
+    // after an abandoned wait: loads that are still under way land (or a limit runs out) before the CTA ends
+    if (abort_s != 0 && threadIdx.x == 0 && (!PAIR || rank == 0)) drain_stages(bar0, asked_s, (uint32_t)kStages);
+    __syncwarp();
     if (PAIR || P.splits > 1) cluster_sync_all();       // no CTA leaves while another may touch its shared memory or TMEM
     if (warp == 1) {
         tc_fence_after();

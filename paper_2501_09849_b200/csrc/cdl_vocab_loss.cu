@@ -156,7 +156,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 {
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 4];
-    __shared__ uint32_t tmem_base_s;
+    __shared__ uint32_t tmem_base_s, asked_s;
     __shared__ int abort_s;
 
     constexpr int kBRows = PAIR ? 128 : 256;           // most columns of a tile that this CTA stages
@@ -196,7 +196,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer (one lane)
         if (lane == 0) {
-            uint32_t st = 0u, par = 1u;
+            uint32_t st = 0u, par = 1u, asked = 0u;
             auto load = [&](uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t fb) {
                 if (PAIR) tma_load_2d_pair(dst, map, c0, c1, fb);
                 else tma_load_2d(dst, map, c0, c1, fb);
@@ -227,6 +227,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 #pragma unroll
                         for (int b = 0; b < kBRows / 64; ++b) load(sb + (uint32_t)b * 8192u, map_b, brow + b * 64, r, fb);
                     } else load(sb, map_b, r, brow, fb);
+                    ++asked;
                     r += kBK;
                     if (!PAIR && r == r1) r = r0;
                     if (++st == (uint32_t)kStages) {
@@ -248,6 +249,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                 else if (GRAD && mode == DH) stages_of(No(), Yes(), map_a, map_b, arow, brow, bytes, u.rb0 * kBK, u.rb1 * kBK);
                 else stages_of(No(), No(), map_a, map_b, arow, brow, bytes, u.rb0 * kBK, u.rb1 * kBK);
             }
+            asked_s = asked;
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (one lane; CTA 0 of a pair)
@@ -507,6 +509,9 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
     }
     tc_fence_before();
     __syncthreads();
+    // after an abandoned wait: loads that are still under way land (or a limit runs out) before the CTA ends
+    if (abort_s != 0 && threadIdx.x == 0 && rank == 0) drain_stages(bar0, asked_s, (uint32_t)kStages);
+    __syncwarp();
     if (PAIR) cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();

@@ -81,4 +81,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// The loads of the last `stages` of `asked` ring stages, whose barriers are at bar + 8 * (stage % stages): waits until they have
+// landed, for at most 10 ms each (a load on its own takes microseconds; one that another CTA never issued does not come).
+__device__ __forceinline__ void drain_stages(uint32_t bar, uint32_t asked, uint32_t stages)
+{
+    for (uint32_t k = asked > stages ? asked - stages : 0u; k < asked; ++k)
+        for (const unsigned long long t0 = global_ns(); !mbar_try_wait(bar + 8u * (k % stages), (k / stages) & 1u) && global_ns() - t0 < 10000000ull;) {}
+}
+
 }  // namespace cdl
