@@ -15,7 +15,9 @@
 // Tiles: 256 x 256 per CTA pair (cta_group::2, as in the index products), or 128 x 128 per CTA where that is estimated to be
 // faster (make_plan).  With few tiles (a short prompt) the reduced dimension is also cut over the CTAs of a cluster, whose
 // partial tiles are added in a fixed order through distributed shared memory: no scratch in global memory, no atomics, one
-// launch.  In pairs the tiles of a last, partly filled round are cut into parts that go through the workspace.  Rows beyond
+// launch.  A last round that would fill the device partly is one sequence of stages, cut into as many runs as there are CTAs
+// (pairs); tiles that runs share are added from the workspace by a second kernel (398 x 2507 x 23585, 20 pair tiles: 43 us
+// against 82 in 80 single tiles; 2304 x 2304 x 4608, 81: 34 against 43; 48 x 139 x 34086: 13.2 against 18.5 over clusters).  Rows beyond
 // M are zero-filled by TMA and cost no memory traffic.
 // Warp roles: warp 0 issues TMA, warp 1 owns TMEM and issues the MMAs, warp 2 fetches scales (four stages at a time, with
 // asynchronous 4-byte copies: handed over stage by stage they cost another barrier per stage, 1062 cycles instead of 930),
@@ -59,10 +61,11 @@ struct Fp8Params {
     int M, N, KB;                   // KB: blocks of 128 along the reduced dimension
     int tiles_i, tiles_j, slots;
     int splits;                     // CTAs of a cluster that share a tile (single-CTA tiles only)
-    // Pair tiles: the first `whole` units are whole tiles; the tiles behind them, too few to fill the device once more, are
-    // cut into tail_splits parts of the reduced dimension, whose sums go to `part`.
-    int whole, tail_splits;
-    float *part;                    // [unit - whole][64 groups of 4 columns][256 rows][4]
+    // The first `whole` tiles are taken as they are.  The stages of the tiles behind them, too few to fill the device once more,
+    // are one sequence, cut into `ranges` runs of `run` stages wherever that falls; a tile that several runs share goes through
+    // `part`, one piece per run r and tile t (counted from `whole`) at r + t.
+    int whole, ranges, run;
+    float *part;                    // [r + t][columns / 4 of a tile][rows of a tile][4]
     int nb;                         // scales of a k-block of B: N, or ceil(N / 128)
     const float *sa, *sb, *bias;
     void *out;
@@ -98,7 +101,8 @@ __device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti
     ti = first + in - tj * rows;
 }
 
-template <bool PAIR, bool BVEC, typename T>
+// RUNS: some tiles are cut into runs of stages (in one kernel with the others, a product of 2048 x 2048 x 256 took 7.1 us, not 6.2).
+template <bool PAIR, bool BVEC, bool RUNS, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
 fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_o, const Fp8Params P)
@@ -106,7 +110,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     extern __shared__ unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 8 + 2 * kScaleSlots];
     __shared__ uint32_t tmem_base_s, asked_s;
-    __shared__ int abort_s;
+    __shared__ int abort_s, span_s[4];
 
     constexpr int kStages = stages(BVEC);
     constexpr int kTN = PAIR ? 256 : 128;
@@ -118,18 +122,38 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t rank = PAIR || P.splits > 1 ? cluster_ctarank() : 0u;
     const int slot = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x / P.splits;
     const int split = PAIR ? 0 : (int)rank;
-    const int units = PAIR ? P.whole + (P.tiles_i * P.tiles_j - P.whole) * P.tail_splits : P.tiles_i * P.tiles_j;
-    // the tile and the k-blocks of a unit
-    auto unit_at = [&](int u, int &ti, int &tj, int &kb0, int &kb1) {
-        int tile = u, part = split, parts = PAIR ? 1 : P.splits;
-        if (PAIR && u >= P.whole) {
-            parts = P.tail_splits;
-            tile = P.whole + (u - P.whole) / parts;
-            part = (u - P.whole) - (tile - P.whole) * parts;
+    // The tiles of a CTA (a pair): slot, slot + slots and so on below `whole`, then those its run of stages touches (kept in
+    // shared memory: the epilogue has no registers to spare).
+    volatile int *span = span_s;                        // the run's stages, its tiles
+    if (RUNS && threadIdx.x == 0) {
+        int lo = 0, hi = 0, tail_first = P.whole, tail_end = P.whole;
+        if (slot < P.ranges) {
+            lo = slot * P.run;
+            hi = min(lo + P.run, (P.tiles_i * P.tiles_j - P.whole) * P.KB);
+            tail_first = P.whole + lo / P.KB;
+            tail_end = P.whole + (hi - 1) / P.KB + 1;
         }
-        tile_at(tile, P.tiles_i, P.tiles_j, ti, tj);
-        kb0 = parts == 1 ? 0 : (int)((long long)P.KB * part / parts);
-        kb1 = parts == 1 ? P.KB : (int)((long long)P.KB * (part + 1) / parts);
+        span[0] = lo;
+        span[1] = hi;
+        span[2] = tail_first;
+        span[3] = tail_end;
+    }
+    auto first_tile = [&] { return !RUNS || slot < P.whole ? slot : span[2]; };
+    auto next_tile = [&](int u) { return !RUNS || u + P.slots < P.whole ? u + P.slots : (u < P.whole ? span[2] : u + 1); };
+    auto end_tile = [&] { return RUNS ? span[3] : P.whole; };
+    // its place, its k-blocks, and where the sums go: a piece, or (-1) the output
+    auto tile_of = [&](int u, int &ti, int &tj, int &kb0, int &kb1, int &piece) {
+        tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
+        const int parts = PAIR || RUNS ? 1 : P.splits;
+        kb0 = parts == 1 ? 0 : (int)((long long)P.KB * split / parts);
+        kb1 = parts == 1 ? P.KB : (int)((long long)P.KB * (split + 1) / parts);
+        piece = -1;
+        if (RUNS && u >= P.whole) {
+            const int first = (u - P.whole) * P.KB;
+            kb0 = max(span[0] - first, 0);
+            kb1 = min(span[1] - first, P.KB);
+            if (kb1 - kb0 < P.KB) piece = slot + u - P.whole;
+        }
     };
 
     const uint32_t bar0 = smem_u32(&bars[0]);
@@ -168,9 +192,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             // ------------------------------------------------------------ TMA producer (one lane)
             if (lane == 0) {
                 uint32_t st = 0u, par = 1u, asked = 0u;
-                for (int u = slot; u < units && !failed; u += P.slots) {
-                    int ti, tj, kb0, kb1;
-                    unit_at(u, ti, tj, kb0, kb1);
+                for (int u = first_tile(); u < end_tile() && !failed; u = next_tile(u)) {
+                    int ti, tj, kb0, kb1, piece;
+                    tile_of(u, ti, tj, kb0, kb1, piece);
                     const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0);
                     const int brow = tj * kTN + (PAIR ? (int)rank * 128 : 0);
                     for (int kb = kb0; kb < kb1; ++kb) {
@@ -205,9 +229,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 // D binary32, A and B e4m3, both K-major
                 const uint32_t idesc = (1u << 4) | ((uint32_t)(kTN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
                 uint32_t st = 0u, par = 0u, buf = 0u, tpar = 1u;
-                for (int u = slot; u < units && !failed; u += P.slots) {
-                    int ti, tj, kb0, kb1;
-                    unit_at(u, ti, tj, kb0, kb1);
+                for (int u = first_tile(); u < end_tile() && !failed; u = next_tile(u)) {
+                    int ti, tj, kb0, kb1, piece;
+                    tile_of(u, ti, tj, kb0, kb1, piece);
                     for (int kb = kb0; kb < kb1; ++kb) {
                         const uint32_t fb = bar0 + 8u * st, tf = tfull0 + 8u * buf, te = tempty0 + 8u * buf;
                         if ((!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs)) ||
@@ -240,9 +264,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             // ------------------------------------------------------------ scales: a stage's row and column scales by
             // asynchronous 4-byte copies (their addresses have no alignment to rely on), several stages ahead
             uint32_t q = 0u, par = 1u;
-            for (int u = slot; u < units && !failed; u += P.slots) {
-                int ti, tj, kb0, kb1;
-                unit_at(u, ti, tj, kb0, kb1);
+            for (int u = first_tile(); u < end_tile() && !failed; u = next_tile(u)) {
+                int ti, tj, kb0, kb1, piece;
+                tile_of(u, ti, tj, kb0, kb1, piece);
                 const int arow = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0), col = tj * kTN;
                 for (int kg = kb0; kg < kb1; kg += kGroup) {
                     const uint32_t sf = sfull0 + 8u * q;
@@ -286,11 +310,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         auto tile_col = [&](int ch) { return group * kCols + ch * 32; };      // of chunk ch of 32 columns
         const uint32_t wbuf = smem_base + (uint32_t)(kStages * kStageBytes) + (uint32_t)((warp - 4) * kOutWarpBytes);
         uint32_t buf = 0u, tpar = 0u, q = 0u, spar = 0u, oblk = 0u;
-        for (int u = slot; u < units && !failed; u += P.slots) {
-            int ti, tj, kb0, kb1;
-            unit_at(u, ti, tj, kb0, kb1);
-            const int row0 = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
-            const int row = row0 + lane;
+        for (int u = first_tile(); u < end_tile() && !failed; u = next_tile(u)) {
+            int ti, tj, kb0, kb1, piece;
+            tile_of(u, ti, tj, kb0, kb1, piece);
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j) acc[j] = make_float2(0.0f, 0.0f);
             int in = 0;                                  // stage of the group
@@ -372,6 +394,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
             }
             if (failed) break;
+            if (RUNS) {                                  // its place is worked out anew instead of being held over the stages
+                asm("" : "+r"(u));
+                tile_of(u, ti, tj, kb0, kb1, piece);
+            }
+            const int row0 = ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
+            const int row = row0 + lane;
             if (!PAIR && P.splits > 1) {
                 // The partial tile, [rows][128] binary32, takes the place of the pipeline's stages: this warp has seen the
                 // last of the CTA's products, so all loads have landed and been read.  16-byte units of a row are
@@ -389,11 +417,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 break;
             }
             if (row0 >= P.M) continue;
-            if (PAIR && u >= P.whole) {
+            if (RUNS && piece >= 0) {
                 // a part of a tile: its sums as they are, four columns of 32 consecutive rows per instruction
-                float4 *q = reinterpret_cast<float4 *>(P.part) + ((long long)(u - P.whole) * 64 + group * (kCols / 4)) * 256 + (int)rank * 128 + quarter * 32 + lane;
+                constexpr int kRows = PAIR ? 256 : 128;
+                float4 *q = reinterpret_cast<float4 *>(P.part) + ((long long)piece * (kTN / 4) + group * (kCols / 4)) * kRows + (PAIR ? (int)rank * 128 : 0) + quarter * 32 + lane;
 #pragma unroll
-                for (int j = 0; j < kCols / 4; ++j) q[j * 256] = make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
+                for (int j = 0; j < kCols / 4; ++j) q[j * kRows] = make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
                 continue;
             }
 #pragma unroll
@@ -513,44 +542,71 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
 }
 
-template <typename T>
-const void *variant(bool pair, bool bvec)
+template <bool PAIR, bool BVEC, bool RUNS>
+const void *variant(int type)
 {
-    if (pair) return bvec ? reinterpret_cast<const void *>(&fp8_gemm_kernel<true, true, T>) : reinterpret_cast<const void *>(&fp8_gemm_kernel<true, false, T>);
-    return bvec ? reinterpret_cast<const void *>(&fp8_gemm_kernel<false, true, T>) : reinterpret_cast<const void *>(&fp8_gemm_kernel<false, false, T>);
+    if (type == CDL_F32) return reinterpret_cast<const void *>(&fp8_gemm_kernel<PAIR, BVEC, RUNS, float>);
+    if (type == CDL_BF16) return reinterpret_cast<const void *>(&fp8_gemm_kernel<PAIR, BVEC, RUNS, __nv_bfloat16>);
+    return reinterpret_cast<const void *>(&fp8_gemm_kernel<PAIR, BVEC, RUNS, __half>);
 }
-const void *variant(int type, bool pair, bool bvec)
+template <bool PAIR, bool BVEC>
+const void *variant(int type, bool runs) { return runs ? variant<PAIR, BVEC, true>(type) : variant<PAIR, BVEC, false>(type); }
+const void *variant(int type, bool pair, bool bvec, bool runs)
 {
-    if (type == CDL_F32) return variant<float>(pair, bvec);
-    return type == CDL_BF16 ? variant<__nv_bfloat16>(pair, bvec) : variant<__half>(pair, bvec);
+    if (pair) return bvec ? variant<true, true>(type, runs) : variant<true, false>(type, runs);
+    return bvec ? variant<false, true>(type, runs) : variant<false, false>(type, runs);
 }
 
-// The tiles that were cut into parts: the parts' sums in their order, the bias, the output type.  One thread per four columns of
-// a row, consecutive threads on consecutive rows (as the parts are stored).
-template <typename T>
-__global__ void __launch_bounds__(256)
-fp8_sum_kernel(const float *part, int parts, int first, int tiles_i, int tiles_j, int M, int N, const float *bias, T *out, long long ldo)
+// The tiles that runs share: their pieces in the order of the runs, the bias, the output type.  A block takes 64 rows x 16 columns:
+// read as the pieces are stored (consecutive threads on consecutive rows), written along rows through shared memory.
+constexpr int kSumRows = 64, kSumCols = 16;
+template <int EDGE, typename T>
+__global__ void __launch_bounds__(kSumRows * kSumCols / 4)
+fp8_sum_kernel(const float *part, int run, int KB, int first, int tiles_i, int tiles_j, int M, int N, const float *bias, T *out, long long ldo)
 {
-    follow_previous();
+    __shared__ float tile[kSumRows][kSumCols + 1];
+    follow_previous();                                  // (also where nothing is left to do: what follows relies on it)
+    const int t = (int)blockIdx.x, r0 = t * KB / run, r1 = ((t + 1) * KB - 1) / run;
+    if (r0 == r1) return;                               // one run had all of it
     int ti, tj;
-    tile_at(first + (int)blockIdx.x, tiles_i, tiles_j, ti, tj);
-    const long long row = (long long)ti * 256 + threadIdx.x;
-    const int col = tj * 256 + (int)blockIdx.y * 4;
-    if (row >= M || col >= N) return;
-    const float4 *q = reinterpret_cast<const float4 *>(part) + ((long long)blockIdx.x * parts * 64 + blockIdx.y) * 256 + threadIdx.x;
-    float4 v = q[0];
-    for (int s = 1; s < parts; ++s) {
-        const float4 w = q[(long long)s * 64 * 256];
-        v.x += w.x;
-        v.y += w.y;
-        v.z += w.z;
-        v.w += w.w;
+    tile_at(first + t, tiles_i, tiles_j, ti, tj);
+    constexpr int kAcross = EDGE / kSumCols;
+    const int rb = (int)blockIdx.y / kAcross * kSumRows, cb = (int)blockIdx.y % kAcross * kSumCols;
+    const long long row0 = (long long)ti * EDGE + rb;
+    const int col0 = tj * EDGE + cb, r = (int)threadIdx.x % kSumRows, c4 = (int)threadIdx.x / kSumRows;
+    if (row0 >= M || col0 >= N) return;
+    if (row0 + r < M) {                                 // (rows beyond M were not stored)
+        const float4 *q = reinterpret_cast<const float4 *>(part) + ((long long)(r0 + t) * (EDGE / 4) + cb / 4 + c4) * EDGE + rb + r;
+        float4 v = q[0];
+#pragma unroll 8
+        for (int k = 1; k <= r1 - r0; ++k) {
+            const float4 w = q[(long long)k * (EDGE / 4) * EDGE];
+            v.x += w.x;
+            v.y += w.y;
+            v.z += w.z;
+            v.w += w.w;
+        }
+        tile[r][c4 * 4] = v.x;
+        tile[r][c4 * 4 + 1] = v.y;
+        tile[r][c4 * 4 + 2] = v.z;
+        tile[r][c4 * 4 + 3] = v.w;
     }
-    const float o4[4] = {v.x, v.y, v.z, v.w};
-    T *o = out + row * ldo + col;
+    __syncthreads();
+    const int c = (int)threadIdx.x % kSumCols;
+    if (col0 + c >= N) return;
+    const float b = bias != nullptr ? __ldg(bias + col0 + c) : 0.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (col + j < N) o[j] = from_f32<T>(o4[j] + (bias != nullptr ? __ldg(bias + col + j) : 0.0f));
+    for (int k = (int)threadIdx.x / kSumCols; k < kSumRows; k += kSumRows / 4)
+        if (row0 + k < M) out[(row0 + k) * ldo + col0 + c] = from_f32<T>(tile[k][c] + b);
+}
+
+template <typename T>
+int launch_sum(bool pair, const Fp8Params &P, cudaStream_t st)
+{
+    const int edge = pair ? 256 : 128;
+    const dim3 grid((unsigned)(P.tiles_i * P.tiles_j - P.whole), (unsigned)((edge / kSumRows) * (edge / kSumCols)));
+    return launch_following(pair ? &fp8_sum_kernel<256, T> : &fp8_sum_kernel<128, T>, grid, dim3(kSumRows * kSumCols / 4), 0, st,
+                            static_cast<const float *>(P.part), P.run, P.KB, P.whole, P.tiles_i, P.tiles_j, P.M, P.N, P.bias, static_cast<T *>(P.out), P.ldo);
 }
 
 // out = bias (or 0) where the reduced dimension is empty
@@ -570,10 +626,11 @@ struct Fp8Plan {
     bool pair;
     int tiles_i, tiles_j;
     int splits;                 // CTAs of a cluster per tile (single-CTA tiles)
-    int whole, tail_splits;     // pair tiles: see Fp8Params
+    int whole, ranges, run;     // see Fp8Params
     size_t part_bytes;
 };
 constexpr int kPlanSms = 148;
+constexpr int64_t kL2Bytes = 126000000;
 constexpr size_t kStatusBytes = 256;
 
 bool make_plan(int32_t M, int32_t N, int32_t K, Fp8Plan *p)
@@ -581,37 +638,41 @@ bool make_plan(int32_t M, int32_t N, int32_t K, Fp8Plan *p)
     const int64_t KB = ((int64_t)K + 127) / 128, pairs = kPlanSms / 2;
     const int64_t pair_tiles = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256), tiles = (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128);
     if (tiles > 0x3fffffff) return false;
-    // Single-CTA tiles: few of them are cut over the CTAs of a cluster.  (Clusters of four and eight do not fit everywhere: the
-    // device runs 32 and 14 of them at once for certain.)
+    // Three forms, each with its estimate in nanoseconds: tiles as they are; with the last, partly filled round cut into runs
+    // that fill the device, which costs the pieces' way through memory and another launch; and, for few tiles of a single CTA,
+    // cut over the CTAs of a cluster.  (Clusters of four and eight do not fit everywhere: the device runs 32 and 14 of them at
+    // once for certain.)
+    struct Form { int64_t ns, whole, ranges, run, splits, piece_bytes; bool pair; } best = {INT64_MAX, 0, 0, 0, 1, 0, false};
+    auto consider = [&](const Form &f) {
+        if (f.ns < best.ns) best = f;
+    };
+    for (int pair = 0; pair < 2; ++pair) {
+        const int64_t slots = pair ? pairs : kPlanSms, n = pair ? pair_tiles : tiles, tail = n % slots, stage = pair ? 550 : 420;
+        const int64_t start = pair ? 5000 : 4000, tile = (pair ? 1200 : 800) + stage * KB, edge = pair ? 256 : 128;
+        consider(Form{start + (n + slots - 1) / slots * tile, n, 0, 0, 1, 0, pair != 0});
+        if (tail > 0) {
+            const int64_t stages = tail * KB, most = stages / 4 < slots ? stages / 4 : slots;        // four stages at least
+            if (most > 1) {
+                const int64_t run = (stages + most - 1) / most, ranges = (stages + run - 1) / run, bytes = (ranges + tail) * edge * edge * 4;
+                // (tiles that run side by side no longer read the same k-blocks at one time: 582 x 5164 x 34907 in pairs 156 us, 147 whole)
+                const int64_t apart = ((int64_t)M + N) * K > kL2Bytes ? stage * run / 10 : 0;
+                consider(Form{start + n / slots * tile + stage * run + apart + (pair ? 3000 : 1000) + 3500 + bytes / 6000 + 30 * (ranges / tail), n - tail, ranges, run, 1, bytes, pair != 0});
+            }
+        }
+    }
     int64_t splits = 1;
     const int64_t clusters[4] = {kPlanSms, pairs, 32, 14};
     for (int i = 1; i < 4 && tiles <= clusters[i] && (2ll << i) <= KB; ++i) splits = 1ll << i;
-    // Whichever form is estimated to be faster, in nanoseconds: a start, a stage (550 and 420: a pair's stage does four times the
-    // work), a tile's output, the sum over a cluster.  Measured both ways: 512 x 4096 x 4096 21.2 us in pairs against 17.5,
-    // 1009 x 2304 x 1000 9.3 against 7.6, 2048 x 2048 x 2048 14.3 against 17.7, 6000 x 3000 x 2000 46.9 against 61.8.
-    const int64_t pair_rounds = (pair_tiles + pairs - 1) / pairs, rounds = splits > 1 ? 1 : (tiles + kPlanSms - 1) / kPlanSms;
-    const int64_t pair_ns = 5000 + pair_rounds * (1200 + 550 * KB), single_ns = 4000 + rounds * (800 + 420 * ((KB + splits - 1) / splits)) + (splits > 1 ? 2000 : 0);
-    p->pair = pair_ns < single_ns;
-    const int edge = p->pair ? 256 : 128;
+    if (splits > 1) consider(Form{4000 + 800 + 420 * ((KB + splits - 1) / splits) + 2000, tiles, 0, 0, splits, 0, false});
+    const int edge = best.pair ? 256 : 128;
+    p->pair = best.pair;
     p->tiles_i = (int)(((int64_t)M + edge - 1) / edge);
     p->tiles_j = (int)(((int64_t)N + edge - 1) / edge);
-    p->splits = p->pair ? 1 : (int)splits;
-    p->tail_splits = 1;
-    p->whole = (int)pair_tiles;
-    p->part_bytes = 0;
-    if (!p->pair || pair_tiles < pairs) return true;
-    // The last, partly filled round: cut its tiles so that the parts fill the device.  A stage takes half a microsecond and the
-    // parts cost their way through memory and a launch, about as much as 24 stages (2304 x 4608 x 50176: 14 tiles of the last
-    // round in 5 parts each, 858 -> 716 us; 2304 x 2304 x 4608, 36 stages, 43 us either way).
-    const int64_t tail = pair_tiles % pairs;
-    if (tail > 0) {
-        const int64_t s = pairs / tail;
-        if (s >= 2 && KB - KB / s >= 32) {
-            p->tail_splits = (int)s;
-            p->whole = (int)(pair_tiles - tail);
-            p->part_bytes = (size_t)tail * (size_t)s * 256 * 256 * sizeof(float);
-        }
-    }
+    p->splits = (int)best.splits;
+    p->whole = (int)best.whole;
+    p->ranges = (int)best.ranges;
+    p->run = (int)best.run;
+    p->part_bytes = (size_t)best.piece_bytes;
     return true;
 }
 }  // namespace
@@ -670,7 +731,8 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     P.tiles_j = plan.tiles_j;
     P.splits = plan.splits;
     P.whole = plan.whole;
-    P.tail_splits = plan.tail_splits;
+    P.ranges = plan.ranges;
+    P.run = plan.run;
     P.part = reinterpret_cast<float *>(static_cast<char *>(ws) + kStatusBytes);
     const int esz = type_bytes(out_type);
     // (a TMA store fills the last 16-byte unit of a row with zeros beyond N: rows that do not end on one are stored directly)
@@ -699,16 +761,16 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     cfg.attrs = at;
     if (!attr_set[dev]) {
         for (int t = 0; t < 3; ++t)
-            for (int v = 0; v < 4; ++v)
-                if (cudaFuncSetAttribute(variant(t, (v & 1) != 0, (v & 2) != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes((v & 2) != 0)) != cudaSuccess) {
+            for (int v = 0; v < 8; ++v)
+                if (cudaFuncSetAttribute(variant(t, (v & 1) != 0, (v & 2) != 0, (v & 4) != 0), cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes((v & 2) != 0)) != cudaSuccess) {
                     (void)cudaGetLastError();
                     return CDL_ERR_LAUNCH;
                 }
         // the pair kernels' shares must fit what a block is launched with, or an epilogue warpgroup would wait for good
         for (int t = 0; t < 3; ++t)
-            for (int v = 0; v < 2; ++v) {
+            for (int v = 0; v < 4; ++v) {
                 cudaFuncAttributes fa;
-                if (cudaFuncGetAttributes(&fa, variant(t, true, v != 0)) != cudaSuccess || fa.numRegs < kRegsLaunch) {
+                if (cudaFuncGetAttributes(&fa, variant(t, true, (v & 1) != 0, (v & 2) != 0)) != cudaSuccess || fa.numRegs < kRegsLaunch) {
                     (void)cudaGetLastError();
                     return CDL_ERR_LAUNCH;
                 }
@@ -719,17 +781,17 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
         cfg.attrs = at + 1;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, variant(CDL_BF16, true, false), &cfg) != cudaSuccess || n < 1) {
+        if (cudaOccupancyMaxActiveClusters(&n, variant(CDL_BF16, true, false, false), &cfg) != cudaSuccess || n < 1) {
             (void)cudaGetLastError();
             n = sms / 2;
         }
         pair_slots[dev] = n < sms / 2 ? n : sms / 2;
         attr_set[dev] = true;
     }
-    const int64_t tiles = (int64_t)P.tiles_i * P.tiles_j;
-    const int64_t units = pair ? P.whole + (tiles - P.whole) * P.tail_splits : tiles;
-    const int64_t dev_slots = pair ? pair_slots[dev] : (P.splits > 1 ? units : sms);
-    P.slots = (int)(units < dev_slots ? units : dev_slots);
+    // (a CTA has one run at most: as many are started as there are runs, should the device have fewer places)
+    const int64_t places = pair ? pair_slots[dev] : (P.splits > 1 ? P.whole : sms);
+    P.slots = (int)(P.whole < places ? P.whole : places);
+    if (P.slots < P.ranges) P.slots = P.ranges;
     at[1].val.clusterDim.x = pair ? 2u : (unsigned)P.splits;
     cfg.attrs = at;
     cfg.gridDim = dim3((pair ? 2u : (unsigned)P.splits) * (unsigned)P.slots);
@@ -737,21 +799,13 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     cfg.stream = st;
     cfg.numAttrs = pair || P.splits > 1 ? 2 : 1;
     void *args[4] = {&map_a, &map_b, &map_o, &P};
-    if (cudaLaunchKernelExC(&cfg, variant(out_type, pair, bvec), args) != cudaSuccess) {
+    if (cudaLaunchKernelExC(&cfg, variant(out_type, pair, bvec, P.ranges > 0), args) != cudaSuccess) {
         (void)cudaGetLastError();
         return CDL_ERR_LAUNCH;
     }
-    if (P.tail_splits > 1) {
-        const dim3 grid((unsigned)(tiles - P.whole), 64);
-        const float *part = P.part;
-        if (out_type == CDL_F32)
-            return launch_following(&fp8_sum_kernel<float>, grid, dim3(256), 0, st, part, P.tail_splits, P.whole, P.tiles_i, P.tiles_j, (int)M, (int)N, bias,
-                                    static_cast<float *>(out), (long long)ldo);
-        if (out_type == CDL_BF16)
-            return launch_following(&fp8_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, part, P.tail_splits, P.whole, P.tiles_i, P.tiles_j, (int)M, (int)N,
-                                    bias, static_cast<__nv_bfloat16 *>(out), (long long)ldo);
-        return launch_following(&fp8_sum_kernel<__half>, grid, dim3(256), 0, st, part, P.tail_splits, P.whole, P.tiles_i, P.tiles_j, (int)M, (int)N, bias,
-                                static_cast<__half *>(out), (long long)ldo);
+    if (P.ranges > 0) {
+        if (out_type == CDL_F32) return launch_sum<float>(pair, P, st);
+        return out_type == CDL_BF16 ? launch_sum<__nv_bfloat16>(pair, P, st) : launch_sum<__half>(pair, P, st);
     }
     return CDL_OK;
 }

@@ -163,6 +163,21 @@ def test_product_with_bias(M, N, K):
         run_matmul(torch, M, N, K, "blocks", out, bias=bias, seed=5)
 
 
+# Few tiles and a long reduced dimension: the tiles' stages are one sequence, cut wherever the runs end.  An entry's sum has at
+# most as many roundings as there are blocks and pieces, and a piece is at least four blocks but for a tile's first and last.
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("M,N,K,pad,offset,out", [
+    (3, 100, 30000, 3, 0, "f32"), (140, 250, 20001, 0, 1, "bf16"), (12, 3720, 9000, 0, 0, "f16"), (257, 1300, 9000, 1, 0, "f16"),
+    (400, 2500, 12300, 0, 0, "bf16"), (1540, 3974, 5000, 2, 0, "f32"), (2301, 2303, 2500, 0, 0, "f32"), (48, 139, 34086, 0, 0, "bf16"),
+])
+def test_product_in_runs(mode, M, N, K, pad, offset, out):
+    import torch
+    bias = torch.randn(N, generator=torch.Generator().manual_seed(M)) * 3 if M % 2 == 0 else None
+    a = run_matmul(torch, M, N, K, mode, out, bias=bias, pad=pad, seed=M + N + K, offset=offset)
+    b = run_matmul(torch, M, N, K, mode, out, bias=bias, pad=pad, seed=M + N + K, offset=offset)
+    assert torch.equal(a, b)
+
+
 def test_product_repeats_and_other_stream():
     import torch
     for M, N, K in ((3, 1000, 4096), (2500, 2400, 640)):
