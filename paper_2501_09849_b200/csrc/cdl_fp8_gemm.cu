@@ -101,6 +101,45 @@ __device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti
     ti = first + in - tj * rows;
 }
 
+__device__ __forceinline__ void store32_if(bool live, char *at, uint32_t v)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p st.global.b32 [%0], %1;\n\t}" ::"l"(at), "r"(v), "r"((uint32_t)live) : "memory");
+}
+__device__ __forceinline__ void store16_if(bool live, char *at, uint32_t v)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p st.global.b16 [%0], %1;\n\t}" ::"l"(at), "h"((unsigned short)v), "r"((uint32_t)live) : "memory");
+}
+
+// A staged piece, 32 rows of 64 bytes, to an output whose rows start anywhere: 16 lanes to a row, four bytes each, and no branch in
+// between (with one per row, which waits for each row's limits, 8207 x 4234 x 223 took 47 us; now 40; entry by entry 74; a row per
+// lane is slower still).  Rows of 16-bit entries that start between two words are staged one entry late: their first word ends
+// with the piece's first entry and begins with the one before it, which the piece on the left has left over (`inner`: there is one).
+template <typename T>
+__device__ __forceinline__ void copy_rows(const Fp8Params &P, uint32_t src, int row0, int c0, bool inner, int lane)
+{
+    const int j = lane & 15, half = lane >> 4, rows = P.M - row0 - half;
+    const int left = P.N - c0 - j * (4 / (int)sizeof(T));                // columns from this lane's entries on
+    char *o = static_cast<char *>(P.out) + ((long long)(row0 + half) * P.ldo + c0) * (long long)sizeof(T) + j * 4;
+    const long long step = 2 * P.ldo * (long long)sizeof(T);             // (a multiple of four bytes: `between` holds for all of a lane's rows)
+    const bool between = sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(o) & 2u) != 0;
+    const bool word = sizeof(T) == 4 ? left >= 1 : (between ? left >= 1 && (inner || j > 0) : left >= 2);
+    const bool single = sizeof(T) == 2 && !between && left == 1;         // an odd last entry
+    if (between) o -= 2;
+#pragma unroll
+    for (int b = 0; b < 2; ++b, o += 8 * step) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = __float_as_uint(lds32(src + (uint32_t)((b * 16 + i * 2 + half) * 64) + ((((uint32_t)j >> 2) ^ ((uint32_t)i & 3u)) << 4) + ((uint32_t)j & 3u) * 4u));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) store32_if(word && b * 16 + i * 2 < rows, o + i * step, w[i]);
+        if (sizeof(T) == 2 && (P.N & 1) != 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) store16_if(single && b * 16 + i * 2 < rows, o + i * step, w[i]);
+        }
+    }
+}
+
 // RUNS: some tiles are cut into runs of stages (in one kernel with the others, a product of 2048 x 2048 x 256 took 7.1 us, not 6.2).
 template <bool PAIR, bool BVEC, bool RUNS, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -425,6 +464,9 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 for (int j = 0; j < kCols / 4; ++j) q[j * kRows] = make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
                 continue;
             }
+            T *row_out = static_cast<T *>(P.out) + (long long)row * P.ldo;
+            const bool late = sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(row_out) & 2u) != 0;       // (see copy_rows)
+            uint32_t before = 0u;
 #pragma unroll
             for (int ch = 0; ch < kCols / 32; ++ch) {
                 const int col0 = tj * kTN + tile_col(ch);
@@ -438,8 +480,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                 }
                 // 64-byte pieces of the warp's 32 rows through its staging block (64-byte swizzle), then by TMA (which clips at the
-                // edges), or, where rows do not start and end on 16 bytes, copied out row by row: consecutive lanes on
-                // consecutive entries (with a row per lane instead, 3000 x 1500 x 5008 took 70 us)
+                // edges), or, where rows do not start and end on 16 bytes, copied out row by row
                 constexpr int kPiece = 64 / (int)sizeof(T);
 #pragma unroll
                 for (int pc = 0; pc < 32 / kPiece; ++pc) {
@@ -454,7 +495,12 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             if constexpr (sizeof(T) == 4) w[j] = __float_as_uint((j & 1) ? a[pc * 8 + c4 * 2 + (j >> 1)].y : a[pc * 8 + c4 * 2 + (j >> 1)].x);
-                            else w[j] = pack2<T>(a[c4 * 4 + j].x, a[c4 * 4 + j].y);
+                            else {
+                                const uint32_t two = pack2<T>(a[c4 * 4 + j].x, a[c4 * 4 + j].y);
+                                w[j] = late ? __funnelshift_r(before, two, 16) : two;
+                                if (c4 == 0 && j == 0 && ch == 0) store16_if(late && row < P.M, reinterpret_cast<char *>(row_out + c0), two);
+                                before = two;
+                            }
                         }
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c4 ^ ((lane >> 1) & 3)) << 4)),
                                      "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
@@ -469,20 +515,13 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         }
                     } else {
                         __syncwarp();
-                        constexpr int kAtOnce = 32 / kPiece;             // rows of an instruction
-                        const int c = lane % kPiece;
-                        const uint32_t unit = (uint32_t)(c * (int)sizeof(T)) >> 4, in = (uint32_t)(c * (int)sizeof(T)) & 15u;
-#pragma unroll 4
-                        for (int r = lane / kPiece; r < 32; r += kAtOnce) {
-                            const uint32_t at = src + (uint32_t)r * 64u + ((unit ^ (((uint32_t)r >> 1) & 3u)) << 4) + in;
-                            if (row0 + r < P.M && c0 + c < P.N) {
-                                T *o = static_cast<T *>(P.out) + (long long)(row0 + r) * P.ldo + c0 + c;
-                                if constexpr (sizeof(T) == 4) *o = lds32(at);
-                                else {
-                                    unsigned short h;
-                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at) : "memory");
-                                    *reinterpret_cast<unsigned short *>(o) = h;
-                                }
+                        copy_rows<T>(P, src, row0, c0, ch > 0, lane);
+                        if constexpr (sizeof(T) == 2) {                  // what the last piece of a late row has left over
+                            const int cols = min(kPiece, P.N - c0);
+                            if (late && row < P.M && (cols & 1) == 0 && (ch == kCols / 32 - 1 || c0 + kPiece >= P.N)) {
+                                uint32_t v = before >> 16;
+                                if (cols < kPiece) v = __float_as_uint(lds32(src + (uint32_t)lane * 64u + ((((uint32_t)cols >> 3) ^ (((uint32_t)lane >> 1) & 3u)) << 4) + (((uint32_t)cols >> 1) & 3u) * 4u));
+                                store16_if(true, reinterpret_cast<char *>(row_out + c0 + cols - 1), v);
                             }
                         }
                         __syncwarp();
