@@ -543,10 +543,11 @@ loss_join_kernel(const float2 *part, int parts, const float *target, const long 
     if (threadIdx.x == 0) {
 #pragma unroll
         for (int k = 1; k < 4; ++k) join(sh[k].x, sh[k].y);
-        const float l = fmaf(m, kLn2, logf(s));
         const long long y = labels[row];
-        lse[row] = l;
-        loss[row] = y >= 0 && y < V ? l - target[row] : 0.0f;
+        lse[row] = fmaf(m, kLn2, logf(s));
+        // (from the logit's distance to the maximum, in the units of the sum: the difference of two rounded numbers of the logits'
+        // size would leave a small loss few right digits)
+        loss[row] = y >= 0 && y < V ? kLn2 * (log2f(s) - fmaf(target[row], kLog2e, -m)) : 0.0f;
     }
 }
 
