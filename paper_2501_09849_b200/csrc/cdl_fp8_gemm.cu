@@ -662,6 +662,7 @@ __global__ void fill_bias_kernel(T *out, long long ldo, long long M, int N, cons
 namespace {
 // What a product of these sizes runs as.  Planned for a B200's 148 SMs so that workspace sizes are fixed.
 struct Fp8Plan {
+    bool rows;                  // few rows of A: the form of its own
     bool pair;
     int tiles_i, tiles_j;
     int splits;                 // CTAs of a cluster per tile (single-CTA tiles)
@@ -703,6 +704,9 @@ bool make_plan(int32_t M, int32_t N, int32_t K, Fp8Plan *p)
     const int64_t clusters[4] = {kPlanSms, pairs, 32, 14};
     for (int i = 1; i < 4 && tiles <= clusters[i] && (2ll << i) <= KB; ++i) splits = 1ll << i;
     if (splits > 1) consider(Form{4000 + 800 + 420 * ((KB + splits - 1) / splits) + 2000, tiles, 0, 0, splits, 0, false});
+    // A few rows take the form that streams B past them, unless this one is clearly faster (rows of B too short for it: 1 x 100000 x
+    // 128 16.0 us there, 11.1 here; 30000 x 500 6.6 and 8.8).
+    p->rows = M <= cdl::kFewRowsFp8 && cdl::plan_fp8_rows(N, K).ns * 85 / 100 <= best.ns;
     const int edge = best.pair ? 256 : 128;
     p->pair = best.pair;
     p->tiles_i = (int)(((int64_t)M + edge - 1) / edge);
@@ -711,7 +715,7 @@ bool make_plan(int32_t M, int32_t N, int32_t K, Fp8Plan *p)
     p->whole = (int)best.whole;
     p->ranges = (int)best.ranges;
     p->run = (int)best.run;
-    p->part_bytes = (size_t)best.piece_bytes;
+    p->part_bytes = p->rows ? 0 : (size_t)best.piece_bytes;
     return true;
 }
 }  // namespace
@@ -748,8 +752,10 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
         else fill_bias_kernel<<<sms * 4, 256, 0, st>>>(static_cast<__half *>(out), ldo, M, N, bias);
         return cudaGetLastError() == cudaSuccess ? CDL_OK : CDL_ERR_LAUNCH;
     }
-    if (M <= kFewRowsFp8)
-        return launch_fp8_rows(A, lda, a_scale, B, ldb, b_scale, b_mode == CDL_FP8_ROWS, M, N, K, out, ldo, out_type, bias, static_cast<int *>(ws), st);
+    Fp8Plan plan;
+    if (!make_plan(M, N, K, &plan)) return CDL_ERR_ARG;
+    if (plan.rows)
+        return launch_fp8_rows(A, lda, a_scale, B, ldb, b_scale, b_mode == CDL_FP8_ROWS, M, N, K, out, ldo, out_type, bias, st);
     Fp8Params P;
     memset(&P, 0, sizeof P);
     P.M = M;
@@ -763,8 +769,6 @@ extern "C" int cdl_fp8_matmul(const void *A, int64_t lda, const float *a_scale, 
     P.out = out;
     P.ldo = ldo;
     P.status = static_cast<int *>(ws);
-    Fp8Plan plan;
-    if (!make_plan(M, N, K, &plan)) return CDL_ERR_ARG;
     const bool pair = plan.pair;
     P.tiles_i = plan.tiles_i;
     P.tiles_j = plan.tiles_j;

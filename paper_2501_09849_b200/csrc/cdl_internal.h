@@ -137,9 +137,14 @@ __device__ __forceinline__ void follow_previous()
 #endif
 
 // Forms of the language-model products for few rows (cdl_fp8_rows.cu, cdl_vocab_rows.cu).
-constexpr int kFewRowsFp8 = 2, kFewRowsLoss = 2;
+constexpr int kFewRowsFp8 = 4, kFewRowsLoss = 2;
+struct Fp8RowsPlan {
+    int warps, slices;              // of a CTA; warps that share the reduced dimension
+    long long blocks, ns;           // CTAs' worth of work; estimated time
+};
+Fp8RowsPlan plan_fp8_rows(int N, int K);
 int launch_fp8_rows(const void *A, long long lda, const float *sa, const void *B, long long ldb, const float *sb, bool b_rows, int M, int N,
-                    int K, void *out, long long ldo, int out_type, const float *bias, int *status, cudaStream_t stream);
+                    int K, void *out, long long ldo, int out_type, const float *bias, cudaStream_t stream);
 int loss_rows_parts(int V);       // partial statistics per row
 int launch_loss_rows(const void *H, long long ldh, const void *W, long long ldw, int type, const long long *labels, int rows, int V, int D,
                      float2 *part, int parts, float *target, int *status, cudaStream_t stream);

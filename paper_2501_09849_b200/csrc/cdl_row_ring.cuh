@@ -25,8 +25,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 // warps would otherwise read the same few memory channels at the same time.
 // The groups of rows of one warp: rows first + i * step .. + kRingRows - 1 for i < groups, bytes [from, to) of each (from a
 // multiple of 16; the last 16-byte unit is fetched whole).
-// BYTES: of each row of a piece.  The two users differ: sixteen warps with 1 KB hide the conversions of 8-bit codes better
-// (9000 x 9000: 21.7 us against 26.5), eight warps with 2 KB read longer runs (32000 x 4096 bf16: 43.9 us against 48.0).
+// BYTES: of each row of a piece (eight warps with 2 KB read longer runs than sixteen with 1 KB: 32000 x 4096 bf16 43.9 us and 48.0).
 template <int WARPS, int BYTES>
 struct RowRing {
     static constexpr int kRingBytes = BYTES;

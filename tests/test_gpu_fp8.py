@@ -178,6 +178,38 @@ def test_product_in_runs(mode, M, N, K, pad, offset, out):
     assert torch.equal(a, b)
 
 
+# One to four rows, whose products a warp does for eight rows of B at a time: ends of the reduced dimension in every 16-byte unit of a
+# block, slices, several passes of a warp.  (A block of 128 is two chains of two matrix instructions: within the four sums
+# that the tolerance has.)
+@pytest.mark.parametrize("mode", list(MODES))
+@pytest.mark.parametrize("M", [1, 2, 3, 4])
+@pytest.mark.parametrize("N,K,pad,offset,out", [(9, 16, 0, 0, "f32"), (131, 531, 1, 0, "bf16"), (8, 1024, 0, 0, "f16"), (1000, 113, 0, 1, "f32"), (77, 9999, 0, 0, "f32"),
+                                                (4099, 640, 2, 0, "bf16"), (20000, 257, 0, 0, "f16")])
+def test_few_rows(mode, M, N, K, pad, offset, out):
+    import torch
+    bias = torch.randn(N, generator=torch.Generator().manual_seed(M)) * 3 if N % 2 else None
+    run_matmul(torch, M, N, K, mode, out, bias=bias, pad=pad, seed=M + N + K, offset=offset)
+
+
+@pytest.mark.parametrize("M", [1, 4, 7])
+def test_codes_that_are_no_numbers_stay_in_their_rows(M):
+    import torch
+    N, K = 50, 400
+    a, sa = operand(torch, M, K, "rows", 1)
+    b, sb = operand(torch, N, K, "blocks", 2)
+    b[13, 390] = torch.tensor(float("nan")).to(torch.float8_e4m3fn)
+    if M > 1:
+        a[M - 1, 5] = torch.tensor(float("nan")).to(torch.float8_e4m3fn)
+    out = torch.zeros(M, N, device="cuda")
+    ws = torch.empty(cdl.cdl_fp8_matmul_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda")
+    cdl.cdl_fp8_matmul(a.cuda(), a.stride(0), sa.cuda(), b.cuda(), b.stride(0), sb.cuda(), MODES["blocks"], M, N, K, out, N, cdl.CDL_F32, None, ws, ws.numel())
+    want = torch.zeros(M, N, dtype=torch.bool)
+    want[:, 13] = True
+    if M > 1:
+        want[M - 1] = True
+    assert torch.equal(out.cpu().isnan(), want)
+
+
 def test_product_repeats_and_other_stream():
     import torch
     for M, N, K in ((3, 1000, 4096), (2500, 2400, 640)):
