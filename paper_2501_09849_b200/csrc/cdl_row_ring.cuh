@@ -23,44 +23,45 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 
 // The pieces of a group are taken from a different one on in every warp (`turn`): with a row pitch that is a power of two all
 // warps would otherwise read the same few memory channels at the same time.
-// The groups of rows of one warp: rows first + i * step .. + kRingRows - 1 for i < groups, bytes [from, to) of each (from a
-// multiple of 16; the last 16-byte unit is fetched whole).
+// The groups of rows of one warp: rows first + i * step .. + kRingRows - 1 for i < groups, the first `bytes` of each (the last
+// 16-byte unit is fetched whole).  Positions in a row are unsigned: a row of 2^30 16-bit entries has 2^31 bytes.
 // BYTES: of each row of a piece (eight warps with 2 KB read longer runs than sixteen with 1 KB: 32000 x 4096 bf16 43.9 us and 48.0).
 template <int WARPS, int BYTES>
 struct RowRing {
-    static constexpr int kRingBytes = BYTES;
+    static constexpr unsigned kRingBytes = BYTES;
     static_assert(WARPS * kRingSlots * kRingRows * BYTES == kRingSmem, "shared memory");
     const unsigned char *base;
     long long pitch, first, step, rows;
-    int groups, from, to, turn;              // turn: byte offset of a group's first piece, a multiple of kRingBytes below to - from
+    int groups;
+    unsigned bytes, turn;                    // turn: byte offset of a group's first piece, a multiple of kRingBytes below `bytes`
     uint32_t smem, bar;                      // this warp's slots and barriers
     volatile int *abort_flag;
     int lane;
-    int next_group, next_at, used, got;      // what is asked for next; slots used so far; pieces taken so far
+    int next_group, used, got;               // what is asked for next; slots used so far; pieces taken so far
+    unsigned next_at;
 
-    __device__ __forceinline__ int after(int at) const { return at + kRingBytes < to ? at + kRingBytes : from; }     // the piece behind one
+    __device__ __forceinline__ unsigned pieces() const { return (bytes + kRingBytes - 1u) / kRingBytes; }            // of a row
+    __device__ __forceinline__ unsigned after(unsigned at) const { return at + kRingBytes < bytes ? at + kRingBytes : 0u; }     // the piece behind one
     __device__ __forceinline__ void ask()    // lane 0: the next piece, if there is one
     {
         if (next_group >= groups) return;
-        const int left = to - next_at, len = left < kRingBytes ? left : kRingBytes;
-        const uint32_t bytes = ((uint32_t)len + 15u) & ~15u, slot = (uint32_t)(used % kRingSlots);
+        const unsigned left = bytes - next_at, len = ((left < kRingBytes ? left : kRingBytes) + 15u) & ~15u;
+        const uint32_t slot = (uint32_t)(used % kRingSlots);
         const uint32_t dst = smem + slot * (kRingRows * kRingBytes), b = bar + 8u * slot;
-        mbar_expect_tx(b, kRingRows * bytes);
+        mbar_expect_tx(b, kRingRows * len);
         const long long r0 = first + next_group * step;
 #pragma unroll
         for (int r = 0; r < kRingRows; ++r)
-            bulk_load(dst + (uint32_t)r * kRingBytes, base + (r0 + r < rows ? r0 + r : rows - 1) * pitch + next_at, bytes, b);
+            bulk_load(dst + (uint32_t)r * kRingBytes, base + (r0 + r < rows ? r0 + r : rows - 1) * pitch + next_at, len, b);
         ++used;
         next_at = after(next_at);
-        if (next_at == from + turn) ++next_group;
+        if (next_at == turn) ++next_group;
     }
     __device__ __forceinline__ void start()
     {
-        next_group = from < to ? 0 : groups;
-        const int pieces = from < to ? (to - from + kRingBytes - 1) / kRingBytes : 1;
-        turn = turn % pieces * kRingBytes;           // (given as a number of pieces)
-        next_at = from + turn;
-        used = got = 0;
+        next_group = used = got = 0;
+        turn = turn % pieces() * kRingBytes;         // (given as a number of pieces)
+        next_at = turn;
         if (lane == 0)
             for (int s = 0; s < kRingSlots; ++s) ask();
     }

@@ -48,6 +48,9 @@ constexpr int kOutWarpBytes = 32 * 128;
 constexpr int kStagesMax = 6;
 constexpr int kSmemBytes = 1024 + kStagesMax * 2 * kBlockBytes + kEpiWarps * kOutWarpBytes;
 constexpr unsigned long long kWaitNs = 2000000000ull;
+// An epilogue's wait is for all stages of a tile, which take up to 0.6 us each (rows that do not start on 128 bytes, under the power
+// cap): 2^24 of them, a reduced dimension of 2^30, are five to ten seconds of valid work.
+constexpr unsigned long long kWaitStageNs = 2000ull;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kStatusBytes = 256;
 
@@ -357,7 +360,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                     if (!(y >= 0 && y < P.V)) label = -2;
                 }
             }
-            if (!__all_sync(0xffffffffu, mbar_try_wait_now(tfull0 + 8u * buf, tpar) || mbar_wait(tfull0 + 8u * buf, tpar, abort_flag, kWaitNs))) {
+            if (!__all_sync(0xffffffffu, mbar_try_wait_now(tfull0 + 8u * buf, tpar) ||
+                                             mbar_wait(tfull0 + 8u * buf, tpar, abort_flag, kWaitNs + kWaitStageNs * (unsigned)(u.rb1 - u.rb0)))) {
                 failed = true;
                 break;
             }

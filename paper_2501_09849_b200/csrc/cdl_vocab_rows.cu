@@ -20,8 +20,8 @@ namespace {
 constexpr int kWords = kRingRows;      // words a warp works on at a time
 constexpr int kWarps = 8;
 using Ring = RowRing<kWarps, 2048>;
-constexpr int kRingBytes = Ring::kRingBytes;
-constexpr int kPieceEntries = kRingBytes / 2;
+constexpr unsigned kRingBytes = Ring::kRingBytes;
+constexpr int kPieceEntries = (int)kRingBytes / 2;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 __device__ __forceinline__ float exp2_fast(float x)
@@ -62,13 +62,12 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
     ringw.step = (long long)gridDim.x * kWarps * kWords;
     ringw.rows = V;
     ringw.groups = ringw.first < V ? (int)((V - 1 - ringw.first) / ringw.step) + 1 : 0;
-    ringw.from = 0;
-    ringw.to = D * 2;
-    ringw.smem = smem_u32(ring) + (uint32_t)(warp * kRingSlots * kRingRows * kRingBytes);
+    ringw.bytes = (unsigned)D * 2u;
+    ringw.smem = smem_u32(ring) + (uint32_t)(warp * kRingSlots * kRingRows) * kRingBytes;
     ringw.bar = smem_u32(&bars[warp * kRingSlots]);
     ringw.abort_flag = &abort_s;
     ringw.lane = lane;
-    ringw.turn = (int)blockIdx.x * kWarps + warp;
+    ringw.turn = blockIdx.x * kWarps + (unsigned)warp;
     ringw.start();
     bool failed = false;
     float m[R], s[R];
@@ -86,8 +85,9 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
         for (int t = 0; t < R; ++t)
 #pragma unroll
             for (int w = 0; w < kWords; ++w) acc[t][w] = 0.0f;
-        for (int at = ringw.turn, left = 2 * D; left > 0; left -= kRingBytes, at = ringw.after(at)) {
-            const int dp = at / 2;
+        unsigned at = ringw.turn;
+        for (unsigned left = ringw.pieces(); left > 0; --left, at = ringw.after(at)) {
+            const int dp = (int)(at / 2u);
             uint32_t piece;
             if (!ringw.take(piece)) {
                 failed = true;
@@ -98,7 +98,7 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
                 float x[kWords][8];
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) {
-                    const uint4 u = lds_u128(piece + (uint32_t)(w * kRingBytes + (d - dp) * 2));
+                    const uint4 u = lds_u128(piece + (uint32_t)w * kRingBytes + (uint32_t)(d - dp) * 2u);
                     unpack2(u.x, x[w][0], x[w][1], T());
                     unpack2(u.y, x[w][2], x[w][3], T());
                     unpack2(u.z, x[w][4], x[w][5], T());

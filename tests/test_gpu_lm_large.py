@@ -93,3 +93,39 @@ def test_dropout_past_four_gigabytes():
     for r in (0, 40000, rows - 3):             # the same rows as calls of their own
         cdl.cdl_dropout(x[r:], ld, None, 0, part, cols, cdl.CDL_BF16, 3, cols, 0.5, 9, 4 + r * cols)
         assert torch.equal(part, y[r:r + 3, :cols])
+
+
+@pytest.mark.parametrize("T,D", [(1, 2 ** 30), (2, 2 ** 30 - 523), (3, 2 ** 30)])
+def test_longest_rows_of_the_vocabulary_loss(T, D):
+    """Rows at the largest reduced dimension: their bytes pass 31 bits, and a tile's stages take longer than the limit of a single wait."""
+    import torch
+    V, pitch = 2, -(-D // 8) * 8
+    g = torch.Generator().manual_seed(D % 1000 + T)
+    at = torch.tensor([0, 1, 2 ** 29 + 7, D - 700, D - 2, D - 1])          # the only entries that are not 0
+    h, w = (torch.zeros(n, pitch, dtype=torch.bfloat16, device="cuda") for n in (T, V))
+    hv, wv = (torch.randn(n, len(at), generator=g).to(torch.bfloat16) for n in (T, V))
+    h[:, at.cuda()], w[:, at.cuda()] = hv.cuda(), wv.cuda()
+    y = (torch.arange(T) % V).cuda()
+    loss, lse = torch.full((T,), -7.0, device="cuda"), torch.full((T,), -7.0, device="cuda")
+    grad = T > 2
+    nb = cdl.cdl_vocab_loss_workspace_bytes(T, V, D, grad)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    cdl.cdl_vocab_loss_fwd(h, pitch, w, pitch, cdl.CDL_BF16, y, T, V, D, loss, lse, ws, nb)
+    cdl.cdl_workspace_status(ws)
+    logits = hv.double() @ wv.double().t()
+    ref = torch.logsumexp(logits, 1)
+    # six products of normal numbers in binary32, exponentials to 2^-21
+    assert float((lse.double().cpu() - ref).abs().max()) < 1e-5
+    assert float((loss.double().cpu() - (ref - logits[torch.arange(T), y.cpu()])).abs().max()) < 1e-5
+    if not grad:
+        return
+    gl = torch.full((T,), 1.0 / T, device="cuda")
+    dh, dw = torch.full_like(h, 9.0), torch.full_like(w, 9.0)
+    cdl.cdl_vocab_loss_bwd(h, pitch, w, pitch, cdl.CDL_BF16, y, lse, gl, T, V, D, dh, pitch, dw, pitch, ws, nb)
+    cdl.cdl_workspace_status(ws)
+    dl = (torch.exp(logits - ref[:, None]) - (torch.arange(V)[None, :] == y.cpu()[:, None]).double()) / T
+    for got, a, b in ((dh, dl, wv.double()), (dw, dl.t(), hv.double())):
+        # two roundings to 16 bits (dl and the result)
+        assert bool(((got[:, at.cuda()].double().cpu() - a @ b).abs() <= 2 * 2.0 ** -8 * (a.abs() @ b.abs())).all())
+        for row in got:
+            assert int(torch.count_nonzero(row[:D])) == int(torch.count_nonzero(row[at.cuda()]))
