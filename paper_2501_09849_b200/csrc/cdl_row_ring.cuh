@@ -78,14 +78,12 @@ struct RowRing {
         __syncwarp();
         if (lane == 0) ask();
     }
-    // Before the CTA ends after an abandoned wait: bulk copies of this warp that are still under way have landed (or the wait
-    // has run out once more).
+    // Before the CTA ends after an abandoned wait: bulk copies of this warp that are still under way have landed (or a limit has
+    // run out for each; the flag that ends the other waits is set by now and does not count here).
     __device__ __forceinline__ void drain()
     {
         __syncwarp();
-        const int asked = __shfl_sync(0xffffffffu, used, 0);
-        for (int k = asked > kRingSlots ? asked - kRingSlots : 0; k < asked; ++k)
-            mbar_wait(bar + 8u * (uint32_t)(k % kRingSlots), (uint32_t)(k / kRingSlots) & 1u, abort_flag, kRingWaitNs);
+        drain_stages(bar, (uint32_t)__shfl_sync(0xffffffffu, used, 0), (uint32_t)kRingSlots);
     }
 };
 
