@@ -475,8 +475,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 if (P.bias != nullptr) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        if (col0 + 2 * j < P.N) a[j].x += __ldg(P.bias + col0 + 2 * j);
-                        if (col0 + 2 * j + 1 < P.N) a[j].y += __ldg(P.bias + col0 + 2 * j + 1);
+                        if (col0 + 2 * j < P.N) a[j].x += P.bias[col0 + 2 * j];
+                        if (col0 + 2 * j + 1 < P.N) a[j].y += P.bias[col0 + 2 * j + 1];
                     }
                 }
                 // 64-byte pieces of the warp's 32 rows through its staging block (64-byte swizzle), then by TMA (which clips at the
@@ -565,7 +565,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             T *o = static_cast<T *>(P.out) + (long long)(ti * 128 + r) * P.ldo + tj * 128 + c;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (c + j < cols) o[j] = from_f32<T>(o4[j] + (P.bias != nullptr ? __ldg(P.bias + tj * 128 + c + j) : 0.0f));
+                if (c + j < cols) o[j] = from_f32<T>(o4[j] + (P.bias != nullptr ? P.bias[tj * 128 + c + j] : 0.0f));
         }
     }
 
@@ -633,7 +633,7 @@ fp8_sum_kernel(const float *part, int run, int KB, int first, int tiles_i, int t
     __syncthreads();
     const int c = (int)threadIdx.x % kSumCols;
     if (col0 + c >= N) return;
-    const float b = bias != nullptr ? __ldg(bias + col0 + c) : 0.0f;
+    const float b = bias != nullptr ? bias[col0 + c] : 0.0f;
 #pragma unroll
     for (int k = (int)threadIdx.x / kSumCols; k < kSumRows; k += kSumRows / 4)
         if (row0 + k < M) out[(row0 + k) * ldo + col0 + c] = from_f32<T>(tile[k][c] + b);

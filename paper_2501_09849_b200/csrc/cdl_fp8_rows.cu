@@ -136,10 +136,10 @@ fp8_rows_kernel(RowsParams P)
 #pragma unroll
             for (int i = 0; i < kBlocks; ++i) {
                 const int kb = min(k0 + i * 128, P.K - 1) >> 7;
-                x[i] = __ldg(reinterpret_cast<const uint4 *>(x_in + min(k0 + i * 128 + k_in, (P.K - 1) & ~15)));
-                s[i] = __ldg(sb + (long long)kb * P.nb);
-                s0[i] = __ldg(P.sa + (long long)kb * M + m_own);
-                s1[i] = __ldg(P.sa + (long long)kb * M + (m0 + 1 < M ? m0 + 1 : m_own));
+                x[i] = *reinterpret_cast<const uint4 *>(x_in + min(k0 + i * 128 + k_in, (P.K - 1) & ~15));
+                s[i] = sb[(long long)kb * P.nb];
+                s0[i] = P.sa[(long long)kb * M + m_own];
+                s1[i] = P.sa[(long long)kb * M + (m0 + 1 < M ? m0 + 1 : m_own)];
             }
             asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
             const uint32_t at = mine + (uint32_t)(slot * kSlotBytes);
@@ -178,7 +178,7 @@ fp8_rows_kernel(RowsParams P)
         const long long n = first + pass * step + g;
         if (slice == 0 && !second && t < kPad / 2 && n < P.N) {
             T *o = static_cast<T *>(P.out) + n;
-            const float b = P.bias != nullptr ? __ldg(P.bias + n) : 0.0f;
+            const float b = P.bias != nullptr ? P.bias[n] : 0.0f;
             if (m0 < M) o[(long long)m0 * P.ldo] = from_f32<T>(acc0 + b);
             if (m0 + 1 < M) o[(long long)(m0 + 1) * P.ldo] = from_f32<T>(acc1 + b);
         }

@@ -108,7 +108,9 @@ struct NextQuant {
 
 // Launches of the language-model operators: a kernel may be set up while the one before it in the stream drains.  Every kernel
 // launched this way calls follow_previous() before its first access to memory that the stream's earlier work may touch;
-// what it is launched behind need not know.
+// what it is launched behind need not know.  Its inputs can still be written while it is already running, so none of them is
+// loaded as read-only data (no __ldg, no __restrict__ on a kernel's pointers): such a load promises that the data does not change
+// during the kernel, and may be moved ahead of the wait.
 template <typename... Args>
 inline int launch_following(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, Args... args)
 {

@@ -40,8 +40,8 @@ __device__ __forceinline__ void join(float &m, float &s, float m2, float s2)
 
 template <int R, typename T>
 __global__ void __launch_bounds__(32 * kWarps, 1)
-loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W, long long ldw, const long long *__restrict__ labels,
-                 int rows, int V, int D, float2 *__restrict__ part, int parts, float *__restrict__ target, int *status)
+loss_rows_kernel(const T *H, long long ldh, const T *W, long long ldw, const long long *labels,
+                 int rows, int V, int D, float2 *part, int parts, float *target, int *status)
 {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ __align__(8) unsigned long long bars[kWarps * kRingSlots];
@@ -110,7 +110,7 @@ loss_rows_kernel(const T *__restrict__ H, long long ldh, const T *__restrict__ W
 #pragma unroll
                 for (int t = 0; t < R; ++t) {
                     float h[8];
-                    const uint4 u = __ldg(reinterpret_cast<const uint4 *>(H + (long long)(t < rows ? t : 0) * ldh + d));
+                    const uint4 u = *reinterpret_cast<const uint4 *>(H + (long long)(t < rows ? t : 0) * ldh + d);
                     unpack2(u.x, h[0], h[1], T());
                     unpack2(u.y, h[2], h[3], T());
                     unpack2(u.z, h[4], h[5], T());
