@@ -461,7 +461,9 @@ size_t cdl_fp8_matmul_workspace_bytes(int32_t M, int32_t N, int32_t K);
  * The backward call takes lse from the forward call and dloss[t] = dL/dloss[t] [dev] (1 / count for a mean; not read where the
  * label is outside) and gives
  *   dl[t,v] = dloss[t] * (exp(l[t,v] - lse[t]) - [v = labels[t]]),   dH = dl W,   dW = dl^T H
- * It goes through the vocabulary in pieces, recomputes each piece's logits and rounds dl, divided by the largest |dloss|, to
+ * lse is the forward call's for the same H and W: where the label's probability is close to 1 its entry is taken as minus the sum of
+ * the other words' probabilities, which is good to binary32, and not as a difference from 1, which would only be good to 2^-24 |lse|.
+ * The call goes through the vocabulary in pieces, recomputes each piece's logits and rounds dl, divided by the largest |dloss|, to
  * 16 bits for the two products.
  *   dH [dev] T x D (pitch lddh), dW [dev] V x D (pitch lddw) of `type`, each nullable; overwritten.
  *   H, W, dH, dW 16-byte aligned, pitches multiples of 8.

@@ -12,6 +12,14 @@
 // two passes is lse, one float per row, and the piece's dl is small enough to stay in L2 between the product that
 // writes it and the two that read it.
 //
+// The label's entry of dl is -g_t sum_{v != y_t} exp(l_tv - lse_t), never exp(l_ty - lse_t) - 1, where that would cancel: lse is a
+// binary32 number of the logits' size, so the difference from 1 is only good to 2^-24 |lse| (a loss of 1e-4 among logits of
+// 25: 0.5 % off, of 300: 10 %).  With one piece, DLOGIT adds up the other probabilities of its columns and loss_label_kernel puts
+// the entry into dl before it is read (2 to 4 us: 16 x 3027 x 1958 40.7 -> 42.9, 777 x 32003 x 1000 228 -> 231).  With several, dl of
+// the first piece is consumed before the last is known: the rows whose label has a probability close to 1 (loss_confident_kernel)
+// are put together, and their other words' sums taken by STATS before the first piece (where there is no such row 9 us: 1024 x 100000
+// x 64 214 -> 225); the other rows' entries are good to 2^-10 as the difference.
+//
 // Tiles: 256 x 256 per CTA pair (cta_group::2), 64 reduced entries (128 bytes) per stage, six stages; two accumulators
 // in TMEM let the epilogue of a tile run beside the products of the next.  Where pairs would leave half of the device idle
 // (few rows, a small vocabulary) the statistics take 128-row tiles of one CTA, narrower ones if need be.  The backward pass
@@ -79,7 +87,13 @@ struct LossParams {
     float2 *part;                   // STATS: (maximum in units of log 2, sum of exponentials relative to it) per row and half tile
     int parts;                      // ... entries per row
     float *target;                  // STATS: the label's logit
+    // STATS of the backward pass: the number of rows, on the device, and the label's own logit left out
+    const int *count;
+    int others_only;
     const float *lse, *dloss;       // DLOGIT
+    float *others;                  // DLOGIT, nullable: per row and half tile, the sum of exponentials without the label's
+    int others_ld;
+    const float *entry;             // DLOGIT, nullable: per row, the label's entry over dloss where it is 0 or less
     const float *scale;             // backward: {S, 1/S}, what dl is stored with
     int first, last;                // DH: first / last piece (last: the output itself is written, unless the job is split)
     float *acc;                     // DH: binary32 sums of the pieces so far, row pitch acc_ld, acc_rows rows per split
@@ -114,18 +128,18 @@ struct LossUnit {
     int j, ti, tj, split, rb0, rb1;     // j < 0: no more
 };
 template <bool GRAD>
-__device__ __forceinline__ LossUnit next_unit(LossWalk &w, const LossParams &P, int slot)
+__device__ __forceinline__ LossUnit next_unit(LossWalk &w, const LossParams &P, int slot, int stats_tiles_i)
 {
     LossUnit u;
     u.j = -1;
     if constexpr (!GRAD) {                                      // one job of whole tiles, taken in turn
         const LossJob &J = P.job[0];
         const int n = w.i * P.slots + slot;
-        if (n >= J.tiles_i * J.tiles_j) return u;
+        if (n >= stats_tiles_i * J.tiles_j) return u;
         ++w.i;
         u.j = 0;
         u.split = 0;
-        tile_at(n, J.tiles_i, J.tiles_j, u.ti, u.tj);
+        tile_at(n, stats_tiles_i, J.tiles_j, u.ti, u.tj);
         u.rb0 = 0;
         u.rb1 = (J.R + kBK - 1) / kBK;
         return u;
@@ -172,6 +186,10 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
     const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
     const int slot = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
 
+    if (!GRAD && P.count != nullptr) {                 // mostly there is no such row
+        follow_previous();
+        if (*P.count == 0) return;
+    }
     const uint32_t bar0 = smem_u32(&bars[0]);
     constexpr uint32_t kEmptyOff = 8u * kStagesMax;
     const uint32_t tfull0 = bar0 + 16u * kStagesMax, tempty0 = tfull0 + 16u;
@@ -195,6 +213,8 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
     const uint32_t tmem_base = tmem_base_s;
     follow_previous();
     bool failed = false;
+    const int stats_rows = GRAD ? 0 : (P.count != nullptr ? *P.count : P.job[0].I);
+    const int stats_tiles_i = GRAD ? 0 : (stats_rows + (PAIR ? 255 : 127)) / (PAIR ? 256 : 128);
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer (one lane)
@@ -241,7 +261,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             };
             LossWalk walk{0, 0};
             while (!failed) {
-                const LossUnit u = next_unit<GRAD>(walk, P, slot);
+                const LossUnit u = next_unit<GRAD>(walk, P, slot, stats_tiles_i);
                 if (u.j < 0) break;
                 const int mode = GRAD ? P.job[u.j].mode : STATS;
                 const CUtensorMap *map_a = &maps.a[u.j], *map_b = &maps.b[u.j];
@@ -290,7 +310,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             };
             LossWalk walk{0, 0};
             while (!failed) {
-                const LossUnit u = next_unit<GRAD>(walk, P, slot);
+                const LossUnit u = next_unit<GRAD>(walk, P, slot, stats_tiles_i);
                 if (u.j < 0) break;
                 const int mode = GRAD ? P.job[u.j].mode : STATS;
                 if (!mbar_try_wait_now(tempty0 + 8u * buf, tpar) && !mbar_wait(tempty0 + 8u * buf, tpar, abort_flag, kWaitNs)) {
@@ -335,10 +355,10 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
         };
         LossWalk walk{0, 0};
         while (!failed) {
-            const LossUnit u = next_unit<GRAD>(walk, P, slot);
+            const LossUnit u = next_unit<GRAD>(walk, P, slot, stats_tiles_i);
             if (u.j < 0) break;
             const int mode = GRAD ? P.job[u.j].mode : STATS;
-            const int I = P.job[u.j].I, J = P.job[u.j].J;
+            const int I = GRAD ? P.job[u.j].I : stats_rows, J = P.job[u.j].J;
             const CUtensorMap *map_o = &maps.o[u.j];
             const int row0 = u.ti * (PAIR ? 256 : 128) + (PAIR ? (int)rank * 128 : 0) + quarter * 32;
             const int wcols = P.job[u.j].tn / 2;         // columns of this warp
@@ -346,7 +366,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
             const int row = row0 + lane;
             // what the epilogue needs of its row, fetched while the products run
             int label = -1;                              // column of the row's label in this tile's matrix, or outside it
-            float lse2 = 0.0f, g = 0.0f;
+            float lse2 = 0.0f, g = 0.0f, entry = 1.0f;
             if ((!GRAD || mode == DLOGIT) && row < I) {
                 const long long y = P.labels[row];
                 const long long c = y - (GRAD ? P.v0 : 0);
@@ -358,6 +378,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                     // (a label outside the vocabulary: no gradient)
                     g = y >= 0 && y < P.V ? P.dloss[row] * P.scale[0] * 5.9604644775390625e-8f : 0.0f;
                     if (!(y >= 0 && y < P.V)) label = -2;
+                    if (P.entry != nullptr) entry = P.entry[row];
                 }
             }
             if (!__all_sync(0xffffffffu, mbar_try_wait_now(tfull0 + 8u * buf, tpar) ||
@@ -388,8 +409,11 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
                                 if (label == c0 + c) {
-                                    tgt = __uint_as_float(v[c]);
-                                    hit = true;
+                                    if (P.others_only) v[c] = 0xff800000u;
+                                    else {
+                                        tgt = __uint_as_float(v[c]);
+                                        hit = true;
+                                    }
                                 }
                         }
                         float cm = __uint_as_float(v[0]);
@@ -413,6 +437,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                         if (hit) P.target[row] = tgt;
                     }
                 } else if (mode == DLOGIT) {
+                    float others = 0.0f;
 #pragma unroll 1
                     for (int ch = 0; ch < wcols / 64; ++ch) {
                         const int c0 = col0 + ch * 64;
@@ -426,10 +451,27 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
                                 v[c] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[c]), kLog2e, -lse2)));
+                            if (P.others != nullptr && c0 + 32 * h + 32 > J) {
+#pragma unroll
+                                for (int c = 0; c < 32; ++c)
+                                    if (c0 + 32 * h + c >= J) v[c] = 0u;           // a column that does not exist
+                            }
                             if (__any_sync(0xffffffffu, (unsigned)(label - (c0 + 32 * h)) < 32u)) {
 #pragma unroll
                                 for (int c = 0; c < 32; ++c)
-                                    if (label == c0 + 32 * h + c) v[c] = __float_as_uint(__uint_as_float(v[c]) - 16777216.0f);
+                                    if (label == c0 + 32 * h + c)
+                                        v[c] = P.others != nullptr ? 0u : __float_as_uint(entry <= 0.0f ? entry * 16777216.0f : __uint_as_float(v[c]) - 16777216.0f);
+                            }
+                            if (P.others != nullptr) {
+                                float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+                                for (int c = 0; c < 32; c += 4) {
+                                    s0 += __uint_as_float(v[c]);
+                                    s1 += __uint_as_float(v[c + 1]);
+                                    s2 += __uint_as_float(v[c + 2]);
+                                    s3 += __uint_as_float(v[c + 3]);
+                                }
+                                others += (s0 + s1) + (s2 + s3);
                             }
 #pragma unroll
                             for (int c = 0; c < 16; ++c) {
@@ -440,6 +482,7 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                         }
                         send(w, map_o, false, c0, row0);
                     }
+                    if (P.others != nullptr && row < I) P.others[(long long)row * P.others_ld + 2 * u.tj + half] = others;
                 } else if (mode == DW || (P.last && P.job[u.j].splits == 1)) {
 #pragma unroll 1
                     for (int ch = 0; ch < 2; ++ch) {
@@ -561,7 +604,7 @@ loss_join_kernel(const float2 *part, int parts, const float *target, const long 
 // (measured on 777 x 32003 x 1000 in binary16: 3.9e-4 of dH's norm without it).  binary16 takes top = 2^14, so that
 // probabilities down to 2^-28 are normal numbers.
 __global__ void __launch_bounds__(1024)
-loss_scale_kernel(const float *dloss, const long long *labels, int T, int V, float top, float *out)
+loss_scale_kernel(const float *dloss, const long long *labels, int T, int V, float top, float *out, int *count)
 {
     __shared__ float sh[32];
     follow_previous();
@@ -583,7 +626,90 @@ loss_scale_kernel(const float *dloss, const long long *labels, int T, int V, flo
             const bool use = m > 7.9e-31f && m < 1.2e30f;
             out[0] = use ? top / m : 1.0f;
             out[1] = use ? m / top : 1.0f;
+            *count = 0;                              // of loss_confident_kernel
         }
+    }
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The labels' entries of dl, one piece: minus the sum of the other words' entries, a warp per row.
+template <typename T>
+__global__ void __launch_bounds__(128)
+loss_label_kernel(const float *others, int parts, const long long *labels, const float *dloss, const float *scale, int rows, int V, T *dl, long long ld)
+{
+    follow_previous();
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const long long y = labels[row];
+    if (y < 0 || y >= V) return;
+    const float g = dloss[row] * scale[0] * 5.9604644775390625e-8f;      // (as DLOGIT has it)
+    float s = 0.0f;
+    for (int i = lane; i < parts; i += 32) s += others[row * parts + i];
+    s = warp_sum(s);
+    if (lane == 0) dl[row * ld + y] = from_f32<T>(-s * g);
+}
+
+// Several pieces: the rows whose label's probability is so close to 1 that its distance, taken from lse, is not good to 2^-10: where
+// the loss is below 2^-12 max(|lse|, 8).  A warp per row multiplies the label's logit out; a row that is one of them is copied
+// behind the others (in any order: no result depends on a row's place).
+template <typename T>
+__global__ void __launch_bounds__(128)
+loss_confident_kernel(const T *H, long long ldh, const T *W, long long ldw, const long long *labels, const float *lse, int rows, int V, int D,
+                      float *entry, int *count, int *index, long long *label, T *copy, long long ldc)
+{
+    follow_previous();
+    const int lane = threadIdx.x & 31;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    if (lane == 0) entry[row] = 1.0f;
+    const long long y = labels[row];
+    if (y < 0 || y >= V) return;
+    const T *h = H + row * ldh, *w = W + y * ldw;
+    float l = 0.0f;
+    for (int d = lane * 8; d < D; d += 256) {
+        float a[8], b[8];
+        load8(h + d, a);
+        load8(w + d, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < D) l = fmaf(a[i], b[i], l);
+    }
+    l = warp_sum(l);
+    const float z = lse[row];
+    if (!(z - l < fmaxf(fabsf(z), 8.0f) * 2.44140625e-4f)) return;
+    int at = 0;
+    if (lane == 0) {
+        at = atomicAdd(count, 1);
+        index[at] = (int)row;
+        label[at] = y;
+    }
+    at = __shfl_sync(0xffffffffu, at, 0);
+    for (int d = lane * 8; d < D; d += 256) *reinterpret_cast<uint4 *>(copy + at * ldc + d) = *reinterpret_cast<const uint4 *>(h + d);
+}
+
+// ... and their entries, from the statistics of the other words: a warp per row, the tiles' sums joined in a fixed order.
+__global__ void __launch_bounds__(128)
+loss_entry_kernel(const float2 *part, int parts, const int *count, const int *index, const float *lse, float *entry)
+{
+    follow_previous();
+    const int lane = threadIdx.x & 31, rows = *count;
+    for (long long i = (long long)blockIdx.x * 4 + (threadIdx.x >> 5); i < rows; i += (long long)gridDim.x * 4) {
+        const int row = index[i];
+        const float z = lse[row];
+        float s = 0.0f;
+        for (int k = lane; k < parts; k += 32) {
+            const float2 p = part[i * parts + k];
+            s += p.y * exp2_fast(fmaf(-z, kLog2e, p.x));
+        }
+        s = warp_sum(s);
+        if (lane == 0) entry[row] = -s;
     }
 }
 
@@ -643,7 +769,14 @@ struct LossPlan {
     bool grad_pair;         // backward: CTA pairs on 256 rows, or single CTAs on 128 where H has no more
     int splits;             // parts of the vocabulary piece that dH's product is cut into
     size_t off_target;      // forward
-    size_t dl_bytes;        // backward: dl of one piece (two of them when there are several pieces)
+    // backward, the labels' entries.  One piece: the sums over the other words, dead before dH's sums, whose place they take.
+    // Several: the entries, ahead of dl, and in dl's place, before the first piece is written, the confident rows: their
+    // indexes, labels, copies and statistics.
+    int others_ld, entry_parts;
+    size_t off_entry, off_index, off_label, off_copy, off_part;
+    long long copy_ld;
+    size_t off_dl;
+    size_t dl_bytes;        // dl of one piece (two of them when there are several pieces)
     size_t off_acc;         // backward: binary32 sums of dH, [splits][acc_rows][acc_ld]
     long long acc_ld;
     int acc_rows;
@@ -701,8 +834,20 @@ LossPlan make_plan(int T, int V, int D)
     if (s > 16) s = 16;
     p.splits = s > 1 ? (int)s : 1;
     p.dl_bytes = up256((size_t)T * (size_t)p.Vp * 2);
-    p.off_acc = kOffData + p.dl_bytes * (p.pieces > 1 ? 2 : 1);
+    p.others_ld = (int)(((long long)V + p.dlogit_tn / 2 - 1) / (p.dlogit_tn / 2));
+    p.entry_parts = (int)(((long long)V + p.stats_tn / 2 - 1) / (p.stats_tn / 2));
+    p.copy_ld = ((long long)D + 7) / 8 * 8;
+    p.off_entry = kOffData;
+    p.off_dl = kOffData + (p.pieces > 1 ? up256((size_t)T * sizeof(float)) : 0);
+    p.off_index = p.off_dl;
+    p.off_label = p.off_index + up256((size_t)T * sizeof(int));
+    p.off_copy = p.off_label + up256((size_t)T * sizeof(long long));
+    p.off_part = p.off_copy + up256((size_t)T * (size_t)p.copy_ld * 2);
+    p.off_acc = p.off_dl + p.dl_bytes * (p.pieces > 1 ? 2 : 1);
     p.bwd_bytes = p.off_acc + (p.pieces > 1 || p.splits > 1 ? up256((size_t)p.splits * (size_t)p.acc_rows * (size_t)p.acc_ld * sizeof(float)) : 0);
+    const size_t before = p.pieces > 1 ? p.off_part + up256((size_t)T * (size_t)p.entry_parts * sizeof(float2))
+                                       : p.off_acc + up256((size_t)T * (size_t)p.others_ld * sizeof(float));
+    if (p.bwd_bytes < before) p.bwd_bytes = before;
     return p;
 }
 
@@ -840,6 +985,40 @@ int launch_join(const float2 *part, int parts, const float *target, const long l
     return launch_following(&loss_join_kernel, dim3((unsigned)T), dim3(128), 0, stream, part, parts, target, labels, V, loss, lse);
 }
 
+// Several pieces: the labels' entries of the rows that need them, before the first piece.
+template <typename E>
+int confident_rows(const LossPlan &p, const void *H, long long ldh, const void *W, long long ldw, const long long *labels, const float *lse, int T, int V, int D,
+                   char *base, int *count, cudaStream_t st)
+{
+    return launch_following(&loss_confident_kernel<E>, dim3((unsigned)(((long long)T + 3) / 4)), dim3(128), 0, st, static_cast<const E *>(H), ldh,
+                            static_cast<const E *>(W), ldw, labels, lse, T, V, D, reinterpret_cast<float *>(base + p.off_entry), count,
+                            reinterpret_cast<int *>(base + p.off_index), reinterpret_cast<long long *>(base + p.off_label), reinterpret_cast<E *>(base + p.off_copy),
+                            p.copy_ld);
+}
+int label_entries(const LossPlan &p, const void *H, long long ldh, const void *W, long long ldw, int type, const long long *labels, const float *lse, int T, int V,
+                  int D, char *base, int *count, cudaStream_t st)
+{
+    int rc = type == CDL_BF16 ? confident_rows<__nv_bfloat16>(p, H, ldh, W, ldw, labels, lse, T, V, D, base, count, st)
+                              : confident_rows<__half>(p, H, ldh, W, ldw, labels, lse, T, V, D, base, count, st);
+    if (rc != CDL_OK) return rc;
+    LossParams P;
+    LossMaps maps;
+    memset(&P, 0, sizeof P);
+    memset(&maps, 0, sizeof maps);
+    P.labels = reinterpret_cast<const long long *>(base + p.off_label);
+    P.V = V;
+    P.count = count;
+    P.others_only = 1;
+    P.part = reinterpret_cast<float2 *>(base + p.off_part);
+    P.parts = p.entry_parts;
+    P.status = reinterpret_cast<int *>(base);
+    if (!add_job(P, maps, type, p.stats_pair, STATS, p.stats_tn, T, V, D, 1, base + p.off_copy, p.copy_ld, W, ldw)) return CDL_ERR_LAUNCH;
+    if ((rc = launch_jobs(p.stats_pair, false, type, maps, P, st)) != CDL_OK) return rc;
+    const int blocks = T < 4 * 148 ? (T + 3) / 4 : 148;
+    return launch_following(&loss_entry_kernel, dim3((unsigned)blocks), dim3(128), 0, st, (const float2 *)P.part, P.parts, (const int *)count,
+                            reinterpret_cast<const int *>(base + p.off_index), lse, reinterpret_cast<float *>(base + p.off_entry));
+}
+
 int check_common(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels, int32_t T, int32_t V, int32_t D)
 {
     if (T < 0 || V < 1 || D < 1 || T > kMostExtent || V > kMostExtent || D > kMostExtent || (type != CDL_BF16 && type != CDL_F16)) return CDL_ERR_ARG;
@@ -925,18 +1104,23 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
     if (dH == nullptr && dW == nullptr) return CDL_OK;
     char *base = static_cast<char *>(ws);
     float *scale = reinterpret_cast<float *>(base + kOffScale), *acc = reinterpret_cast<float *>(base + p.off_acc);
-    if ((rc = launch_following(&loss_scale_kernel, dim3(1), dim3(1024), 0, st, dloss, reinterpret_cast<const long long *>(labels), (int)T, (int)V,
-                               type == CDL_F16 ? 16384.0f : 1.0f, scale)) != CDL_OK)
+    const long long *y = reinterpret_cast<const long long *>(labels);
+    int *count = reinterpret_cast<int *>(base + kOffScale) + 2;
+    if ((rc = launch_following(&loss_scale_kernel, dim3(1), dim3(1024), 0, st, dloss, y, (int)T, (int)V, type == CDL_F16 ? 16384.0f : 1.0f, scale, count)) != CDL_OK)
         return rc;
     LossParams P;
     LossMaps maps;
+    if (p.pieces > 1 && (rc = label_entries(p, H, ldh, W, ldw, type, y, lse, T, V, D, base, count, st)) != CDL_OK) return rc;
     // Launch k works on two pieces at a time: the products that read dl of piece k, and dl of piece k + 1 (into the other
     // buffer).  One launch of mixed units has one ragged end where three would have three.
     for (int k = -1; k < p.pieces; ++k) {
         memset(&P, 0, sizeof P);
         memset(&maps, 0, sizeof maps);
-        P.labels = reinterpret_cast<const long long *>(labels);
+        P.labels = y;
         P.V = V;
+        P.entry = p.pieces > 1 ? reinterpret_cast<const float *>(base + p.off_entry) : nullptr;
+        P.others = p.pieces > 1 ? nullptr : acc;
+        P.others_ld = p.others_ld;
         P.lse = lse;
         P.dloss = dloss;
         P.scale = scale;
@@ -953,7 +1137,7 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
         bool ok = true;
         if (k >= 0) {
             const int v0 = k * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
-            const void *dl = base + kOffData + (size_t)(k & 1) * p.dl_bytes;
+            const void *dl = base + p.off_dl + (size_t)(k & 1) * p.dl_bytes;
             if (dH != nullptr) {
                 const bool direct = P.last && p.splits == 1;
                 P.out_h = dH;
@@ -974,10 +1158,18 @@ extern "C" int cdl_vocab_loss_bwd(const void *H, int64_t ldh, const void *W, int
             const int v0 = (k + 1) * p.Vp, words = V - v0 < p.Vp ? V - v0 : p.Vp;
             P.v0 = v0;
             ok = ok && add_job(P, maps, type, p.grad_pair, DLOGIT, p.dlogit_tn, T, words, D, 1, H, ldh, static_cast<const char *>(W) + (size_t)v0 * (size_t)ldw * 2, ldw);
-            ok = ok && set_output(maps, P.jobs - 1, type, base + kOffData + (size_t)((k + 1) & 1) * p.dl_bytes, (uint64_t)words, (uint64_t)T, p.Vp);
+            ok = ok && set_output(maps, P.jobs - 1, type, base + p.off_dl + (size_t)((k + 1) & 1) * p.dl_bytes, (uint64_t)words, (uint64_t)T, p.Vp);
         }
         if (!ok) return CDL_ERR_LAUNCH;
         if ((rc = launch_jobs(p.grad_pair, true, type, maps, P, st)) != CDL_OK) return rc;
+        if (k < 0 && p.pieces == 1) {
+            const dim3 grid((unsigned)(((long long)T + 3) / 4));
+            rc = type == CDL_BF16 ? launch_following(&loss_label_kernel<__nv_bfloat16>, grid, dim3(128), 0, st, (const float *)acc, p.others_ld, y, dloss, (const float *)scale,
+                                                     (int)T, (int)V, reinterpret_cast<__nv_bfloat16 *>(base + p.off_dl), (long long)p.Vp)
+                                  : launch_following(&loss_label_kernel<__half>, grid, dim3(128), 0, st, (const float *)acc, p.others_ld, y, dloss, (const float *)scale,
+                                                     (int)T, (int)V, reinterpret_cast<__half *>(base + p.off_dl), (long long)p.Vp);
+            if (rc != CDL_OK) return rc;
+        }
     }
     if (dH != nullptr && p.splits > 1) {
         const long long units = (long long)T * ((D + 7) / 8);
