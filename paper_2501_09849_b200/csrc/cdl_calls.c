@@ -21,10 +21,11 @@ static struct {
 static PyObject *raw_stream, *current_device;       /* callables of torch, None without a device */
 static PyObject *s_data_ptr, *s_cuda_stream;
 
-/* Each conversion leaves an exception set on failure; the calls test for one once, before the library is entered. */
+/* Each conversion leaves an exception set on failure, and the ones behind it do nothing: most of them can run Python code, which must
+ * not see an exception pending.  The calls test for one before the library is entered. */
 static void *ptr(PyObject *o)
 {
-    if (o == Py_None) return NULL;
+    if (o == Py_None || PyErr_Occurred()) return NULL;
     if (PyLong_Check(o)) return (void *)(uintptr_t)PyLong_AsUnsignedLongLong(o);
     PyObject *r = PyObject_CallMethodNoArgs(o, s_data_ptr);
     if (r == NULL) return NULL;
@@ -34,6 +35,7 @@ static void *ptr(PyObject *o)
 }
 static void *stream(PyObject *o)
 {
+    if (PyErr_Occurred()) return NULL;
     if (o == Py_None) {
         if (raw_stream == NULL || raw_stream == Py_None) return NULL;
         PyObject *d = PyObject_CallNoArgs(current_device);
@@ -52,10 +54,12 @@ static void *stream(PyObject *o)
     Py_DECREF(r);
     return p;
 }
-static int64_t i64(PyObject *o) { return (int64_t)PyLong_AsLongLong(o); }
-static uint64_t u64(PyObject *o) { return (uint64_t)PyLong_AsUnsignedLongLongMask(o); }
+static int64_t i64(PyObject *o) { return PyErr_Occurred() ? 0 : (int64_t)PyLong_AsLongLong(o); }
+static uint64_t u64(PyObject *o) { return PyErr_Occurred() ? 0 : (uint64_t)PyLong_AsUnsignedLongLongMask(o); }
+static double f64(PyObject *o) { return PyErr_Occurred() ? 0.0 : PyFloat_AsDouble(o); }
 static int32_t i32(PyObject *o)
 {
+    if (PyErr_Occurred()) return 0;
     const long v = PyLong_AsLong(o);
     if ((v > INT32_MAX || v < INT32_MIN) && !PyErr_Occurred()) PyErr_SetString(PyExc_OverflowError, "argument does not fit 32 bits");
     return (int32_t)v;
@@ -87,7 +91,7 @@ static PyObject *py_dropout(ARGS)
     void *y = ptr(a[4]), *st = stream(a[12]);
     const int64_t ldx = i64(a[1]), ldr = i64(a[3]), ldy = i64(a[5]), rows = i64(a[7]), cols = i64(a[8]);
     const int32_t type = i32(a[6]);
-    const double p = PyFloat_AsDouble(a[9]);
+    const double p = f64(a[9]);
     const uint64_t seed = u64(a[10]), first = u64(a[11]);
     FINISH(fn.dropout(x, ldx, res, ldr, y, ldy, type, rows, cols, (float)p, seed, first, st));
 }
