@@ -376,7 +376,11 @@ def _calls():
     if _CALLS is None:
         lib = load_library()
         import torch
-        from . import _cdl_calls
+        try:
+            from . import _cdl_calls
+        except ImportError as e:
+            raise RuntimeError("the compiled part of the binding is missing: build it with `python -m paper_2501_09849_b200.build`, which needs "
+                               "a C compiler and the headers of this Python") from e
         raw = device = None
         if torch.cuda.is_available():       # (no device: the call fails in the library, not here)
             torch.cuda.init()
