@@ -2,7 +2,7 @@
 residual connection, and the cross entropy over a vocabulary, forward and backward.
 
 Like layer.CdlLayerStep this module only owns device buffers and issues the calls in order on one stream (recordable into a
-CUDA graph); every number is produced by the kernels behind the ABI.
+CUDA graph); every number but the bias' gradient is produced by the kernels behind the ABI.
 
 Step (x: T x D hidden states, labels: T words, W1: D x D layer weights in binary32, W2: V x D output weights):
    1  W1 -> e4m3 codes, a scale per 128 x 128 block, both orientations               cdl_fp8_quantize
@@ -15,7 +15,8 @@ Step (x: T x D hidden states, labels: T words, W1: D x D layer weights in binary
    8  dY -> codes along rows and along tokens                                           cdl_fp8_quantize
    9  dX = dY W1 (W1's transposed codes), then + dH of the residual connection          cdl_fp8_matmul, cdl_dropout with p = 0
   10  dW1 = dY^T X                                                                      cdl_fp8_matmul
-The gradient of the bias (the column sums of dY) and the optimizer are outside.
+  11  db1 = column sums of dY, with a bias                                                torch.sum
+The optimizer is outside.
 
 ``python -m paper_2501_09849_b200.head`` trains such a head on a synthetic task for a few steps and prints the loss.
 """
@@ -55,6 +56,7 @@ class HeadStep:
         self.loss, self.lse = empty((T,), f32), empty((T,), f32)
         self.dh, self.dy, self.dx = empty((T, D), bf16), empty((T, D), bf16), empty((T, D), bf16)
         self.dw1, self.dw2 = empty((D, D), f32), empty((V, D), bf16)
+        self.db1 = empty((D,), f32) if bias else None
         self.ws_bytes = max(cdl.cdl_fp8_matmul_workspace_bytes(T, D, D), cdl.cdl_fp8_matmul_workspace_bytes(D, D, T),
                             cdl.cdl_vocab_loss_workspace_bytes(T, V, D, True))
         self.ws = empty((self.ws_bytes,), t.uint8)
@@ -76,6 +78,8 @@ class HeadStep:
         cdl.cdl_fp8_matmul(self.gc, pd, self.gs, self.w1ct, pd, self.w1st, blocks, T, D, D, self.dx, D, bf16, **ws)
         cdl.cdl_dropout(self.dx, D, self.dh, D, self.dx, D, bf16, T, D, 0.0, self.seed)
         cdl.cdl_fp8_matmul(self.gct, pt, self.gst, self.xct, pt, self.xst, rows, D, D, T, self.dw1, D, f32, **ws)
+        if self.db1 is not None:
+            self.torch.sum(self.dy, 0, dtype=self.torch.float32, out=self.db1)
 
     def capture(self):
         """Records one step into a CUDA graph and returns it.  A replay draws the same dropout again: this is for a step whose
