@@ -46,14 +46,13 @@ constexpr int kStageBytes = 2 * kBlockBytes;
 constexpr int kOutBytes = 32 * 64;                     // output staging block of a warp: 32 rows x 64 bytes
 constexpr int kOutBlocks = 2;                          // ... of which a warp has as many stores in flight
 constexpr int kOutWarpBytes = kOutBlocks * kOutBytes;
-constexpr int kStagesMax = 6;
+constexpr int kStages = 5;
 constexpr int kGroup = 4;                              // stages whose scales are handed over together
 constexpr int kScaleSlots = 4;                         // groups on their way or in use
-__host__ __device__ constexpr int stages(bool bvec) { return bvec ? 5 : 5; }
 __host__ __device__ constexpr int slot_floats(bool bvec) { return bvec ? 128 + 256 : 128 + 4; }      // scales of a stage: rows, then columns
 __host__ __device__ constexpr int smem_bytes(bool bvec)
 {
-    return 1024 + stages(bvec) * kStageBytes + kEpiWarps * kOutWarpBytes + kScaleSlots * kGroup * slot_floats(bvec) * 4;
+    return 1024 + kStages * kStageBytes + kEpiWarps * kOutWarpBytes + kScaleSlots * kGroup * slot_floats(bvec) * 4;
 }
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
@@ -90,15 +89,6 @@ __device__ __forceinline__ float4 lds128(uint32_t addr)
     float4 v;
     asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
-}
-
-// Tiles in bands of eight tile rows, columns outer, so that what runs at one time shares operand blocks in L2.
-__device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti, int &tj)
-{
-    const int band = 8 * tiles_j;
-    const int b = u / band, first = b * 8, rows = min(8, tiles_i - first), in = u - b * band;
-    tj = in / rows;
-    ti = first + in - tj * rows;
 }
 
 __device__ __forceinline__ void store32_if(bool live, char *at, uint32_t v)
@@ -147,11 +137,10 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const __grid_constant__ CUtensorMap map_o, const Fp8Params P)
 {
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) unsigned long long bars[2 * kStagesMax + 8 + 2 * kScaleSlots];
+    __shared__ __align__(8) unsigned long long bars[2 * kStages + 8 + 2 * kScaleSlots];
     __shared__ uint32_t tmem_base_s, asked_s;
     __shared__ int abort_s, span_s[4];
 
-    constexpr int kStages = stages(BVEC);
     constexpr int kTN = PAIR ? 256 : 128;
     constexpr int kBufs = 512 / kTN;                   // TMEM buffers of a partial tile
     constexpr int kCols = kTN / 2;                     // columns of an epilogue warp
@@ -196,8 +185,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     };
 
     const uint32_t bar0 = smem_u32(&bars[0]);
-    constexpr uint32_t kEmptyOff = 8u * kStagesMax;
-    const uint32_t tfull0 = bar0 + 16u * kStagesMax, tempty0 = tfull0 + 32u;
+    constexpr uint32_t kEmptyOff = 8u * kStages;
+    const uint32_t tfull0 = bar0 + 16u * kStages, tempty0 = tfull0 + 32u;
     const uint32_t sfull0 = tempty0 + 32u;              // scales of a stage are there; taken: + 8 kScaleSlots
     if (threadIdx.x == 0) {
         abort_s = 0;

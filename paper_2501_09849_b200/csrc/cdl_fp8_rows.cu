@@ -65,13 +65,6 @@ __device__ __forceinline__ void copy16_async(uint32_t dst, const unsigned char *
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(max(0, min(16, live))) : "memory");
 }
-__device__ __forceinline__ uint4 lds_u128(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-
 template <int M, typename T>
 __global__ void __launch_bounds__(32 * kWarps, 1)
 fp8_rows_kernel(RowsParams P)

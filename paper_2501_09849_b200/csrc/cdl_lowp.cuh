@@ -1,4 +1,4 @@
-// Element types of the operators that take 32- and 16-bit floats (CDL_F32, CDL_BF16, CDL_F16): conversions, eight-element
+// Element types of the operators that take 32- and 16-bit floats (CDL_F32, CDL_BF16, CDL_F16): conversions, 16-byte and eight-element
 // accesses, and the argument checks they have in common.
 #pragma once
 #include <cuda_bf16.h>
@@ -56,6 +56,13 @@ __device__ __forceinline__ void unpack2(uint32_t w, float &lo, float &hi, __half
     const float2 f = __half22float2(h);
     lo = f.x;
     hi = f.y;
+}
+
+__device__ __forceinline__ uint4 lds_u128(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
 }
 
 // Eight consecutive elements at a 16-byte boundary.  The loads are evict-first: the operators read each input once.

@@ -87,11 +87,4 @@ struct RowRing {
     }
 };
 
-__device__ __forceinline__ uint4 lds_u128(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-
 }  // namespace cdl

@@ -210,6 +210,15 @@ __device__ __forceinline__ void tmem_free_all(uint32_t base)
     else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(512u) : "memory");
 }
 
+// Tiles in bands of eight tile rows, columns outer, so that what runs at one time shares operand blocks in L2.
+__device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti, int &tj)
+{
+    const int band = 8 * tiles_j;
+    const int b = u / band, first = b * 8, rows = min(8, tiles_i - first), in = u - b * band;
+    tj = in / rows;
+    ti = first + in - tj * rows;
+}
+
 // acc.{x,y} += v.{x,y} * s.{x,y}, two binary32 fused multiply-adds in one instruction
 __device__ __forceinline__ void fma2(float2 &acc, uint32_t v0, uint32_t v1, float2 s)
 {

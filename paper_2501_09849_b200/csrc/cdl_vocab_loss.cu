@@ -37,6 +37,7 @@
 
 #include "cdl_internal.h"
 #include "cdl_lowp.cuh"
+#include "cdl_softmax.cuh"
 #include "cdl_tc.cuh"
 #include "cdl_wait.cuh"
 
@@ -59,7 +60,7 @@ constexpr unsigned long long kWaitNs = 2000000000ull;
 // An epilogue's wait is for all stages of a tile, which take up to 0.6 us each (rows that do not start on 128 bytes, under the power
 // cap): 2^24 of them, a reduced dimension of 2^30, are five to ten seconds of valid work.
 constexpr unsigned long long kWaitStageNs = 2000ull;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr size_t kStatusBytes = 256;
 
 constexpr int kMaxSlots = 160;                         // CTAs, or pairs of them, of a backward launch (148 or 74 on a B200)
@@ -104,21 +105,6 @@ struct LossParams {
     int out_cols;                   // ... of which TMA stores these columns, the threads the few behind them
     int *status;
 };
-
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ void tile_at(int u, int tiles_i, int tiles_j, int &ti, int &tj)
-{
-    const int band = 8 * tiles_j;
-    const int b = u / band, first = b * 8, rows = min(8, tiles_i - first), in = u - b * band;
-    tj = in / rows;
-    ti = first + in - tj * rows;
-}
 
 // The units of a slot, in order.
 struct LossWalk {
@@ -573,23 +559,17 @@ loss_join_kernel(const float2 *part, int parts, const float *target, const long 
     const long long row = blockIdx.x;
     const float2 *p = part + row * parts;
     float m = -INFINITY, s = 0.0f;
-    auto join = [&](float m2, float s2) {
-        const float mn = fmaxf(m, m2);
-        if (mn != -INFINITY) s = s * exp2_fast(m - mn) + s2 * exp2_fast(m2 - mn);
-        else s += s2;                                // (no maximum: 0, or NaN where a logit is NaN)
-        m = mn;
-    };
-    for (int i = threadIdx.x; i < parts; i += 128) join(p[i].x, p[i].y);
+    for (int i = threadIdx.x; i < parts; i += 128) join_stats(m, s, p[i].x, p[i].y);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-        join(m2, s2);
+        join_stats(m, s, m2, s2);
     }
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = make_float2(m, s);
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-        for (int k = 1; k < 4; ++k) join(sh[k].x, sh[k].y);
+        for (int k = 1; k < 4; ++k) join_stats(m, s, sh[k].x, sh[k].y);
         const long long y = labels[row];
         lse[row] = fmaf(m, kLn2, logf(s));
         // (from the logit's distance to the maximum, in the units of the sum: the difference of two rounded numbers of the logits'

@@ -13,6 +13,7 @@
 #include "cdl_internal.h"
 #include "cdl_lowp.cuh"
 #include "cdl_row_ring.cuh"
+#include "cdl_softmax.cuh"
 
 namespace cdl {
 namespace {
@@ -22,21 +23,6 @@ constexpr int kWarps = 8;
 using Ring = RowRing<kWarps, 2048>;
 constexpr unsigned kRingBytes = Ring::kRingBytes;
 constexpr int kPieceEntries = (int)kRingBytes / 2;
-constexpr float kLog2e = 1.44269504088896340736f;
-
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ void join(float &m, float &s, float m2, float s2)
-{
-    const float mn = fmaxf(m, m2);
-    if (mn != -INFINITY) s = s * exp2_fast(m - mn) + s2 * exp2_fast(m2 - mn);
-    else s += s2;
-    m = mn;
-}
 
 template <int R, typename T>
 __global__ void __launch_bounds__(32 * kWarps, 1)
@@ -158,7 +144,7 @@ loss_rows_kernel(const T *H, long long ldh, const T *W, long long ldw, const lon
     if (threadIdx.x < R && (int)threadIdx.x < rows) {
         float mm = sh[0][threadIdx.x].x, ss = sh[0][threadIdx.x].y;
 #pragma unroll
-        for (int k = 1; k < kWarps; ++k) join(mm, ss, sh[k][threadIdx.x].x, sh[k][threadIdx.x].y);
+        for (int k = 1; k < kWarps; ++k) join_stats(mm, ss, sh[k][threadIdx.x].x, sh[k][threadIdx.x].y);
         part[(long long)threadIdx.x * parts + blockIdx.x] = make_float2(mm, ss);
     }
 }
