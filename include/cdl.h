@@ -435,7 +435,7 @@ int cdl_fp8_quantize(const void *x, int64_t ldx, int32_t type, int32_t rows, int
 /*
  * Product of two block-scaled 8-bit matrices, reduced along their rows:
  *   out[m,n] = sum_kb sa(kb,m) * sb(kb,n) * ( sum_{k in block kb} A[m,k] * B[n,k] )  (+ bias[n])
- * blocks of 128 along k; all sums in binary32, rounded once to out_type.  With codes from cdl_fp8_quantize:
+ * blocks of 128 along k, the two scales multiplied first; all sums in binary32, rounded once to out_type.  With codes from cdl_fp8_quantize:
  *   forward          Y[tokens, out]  = X W^T     A = X (rows),        B = W (blocks or rows)
  *   data gradient    dX[tokens, in]  = dY W      A = dY (rows),       B = W transposed (blocks)
  *   weight gradient  dW[out, in]     = dY^T X    A = dY transposed,   B = X transposed (both rows, groups along tokens)
@@ -457,17 +457,19 @@ size_t cdl_fp8_matmul_workspace_bytes(int32_t M, int32_t N, int32_t K);
  *   l[t,v] = sum_d H[t,d] W[v,d],   lse[t] = log sum_v exp l[t,v],   loss[t] = lse[t] - l[t, labels[t]]
  * A label outside 0..V-1 marks a position without a loss: loss[t] = 0 and no gradient (lse[t] is still written).
  *   H [dev] T x D, W [dev] V x D of `type` (CDL_BF16 or CDL_F16), pitches ldh, ldw;  labels [dev] T int64;
- *   loss, lse [dev] T floats.  Products and sums in binary32.
+ *   loss, lse [dev] T floats.  Products and sums in binary32; from three positions on the tensor cores' sums of a logit are cut off, not
+ *   rounded (relative error of the loss 1.1e-6 at D = 2064, 2e-6 at 3269).
  * The backward call takes lse from the forward call and dloss[t] = dL/dloss[t] [dev] (1 / count for a mean; not read where the
  * label is outside) and gives
  *   dl[t,v] = dloss[t] * (exp(l[t,v] - lse[t]) - [v = labels[t]]),   dH = dl W,   dW = dl^T H
  * lse is the forward call's for the same H and W: where the label's probability is close to 1 its entry is taken as minus the sum of
  * the other words' probabilities, which is good to binary32, and not as a difference from 1, which would only be good to 2^-24 |lse|.
  * The call goes through the vocabulary in pieces, recomputes each piece's logits and rounds dl, divided by the largest |dloss|, to
- * 16 bits for the two products.
+ * 16 bits for the two products (in binary16 in steps of 2^-38 of the largest |dloss| at least).
  *   dH [dev] T x D (pitch lddh), dW [dev] V x D (pitch lddw) of `type`, each nullable; overwritten.
  *   H, W, dH, dW 16-byte aligned, pitches multiples of 8.
- *   ws [dev]: cdl_vocab_loss_workspace_bytes(T, V, D, with_gradient) bytes, 256-byte aligned (the larger size serves both).
+ *   ws [dev]: cdl_vocab_loss_workspace_bytes(T, V, D, with_gradient) bytes, 256-byte aligned (the larger size serves both): of the
+ *   order of T V / 16 bytes forward (partial statistics), max(64 MB, 4096 T) for each of two pieces of dl and 4 T D backward.
  * T = 0 is valid (dW is cleared); V and D at least 1.  The results have a fixed order of summation.
  */
 int cdl_vocab_loss_fwd(const void *H, int64_t ldh, const void *W, int64_t ldw, int32_t type, const int64_t *labels,

@@ -6,9 +6,10 @@
 // of four to five cycles each per scheduler and 18 three-input logic operations for four elements.  One thread handles
 // eight consecutive elements (two blocks, one or two 16-byte accesses per tensor) and fetches the next eight while it draws
 // these; the comparison with p is one unsigned comparison of the raw word, the kept value, the scale and the residual are one
-// fused multiply-add under its predicate, and the round keys are kernel parameters.  32749 x 2304: bf16 with residual 81 us
-// (5.6 TB/s), without 79 us (3.8 TB/s, the multiplies), f32 with residual 147 us (6.2 TB/s); four CTAs of 256 threads per SM
-// (five: 92, 80, 165 us, with the same loop before the keys were parameters).
+// fused multiply-add under its predicate, and the round keys are kernel parameters.  32749 x 2304: bf16 with residual 78 to 89 us
+// (5.1 to 5.8 TB/s), without 79 to 86 us (3.5 to 3.8 TB/s, the multiplies), f32 with residual 147 us (6.2 TB/s); four CTAs of 256
+// threads per SM (five: 92, 80, 165 us, with the same loop before the keys were parameters).  A padded tensor has rows of their own,
+// which do not fill the blocks evenly: 2304 columns of pitch 2312 218 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -130,7 +131,8 @@ dropout_vec_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y,
     }
 }
 
-// Any alignment, pitch and first index: a thread takes the (up to four) elements of a row that share a Philox block.
+// Any alignment, pitch and first index: a thread takes the (up to four) elements of a row that share a Philox block, one at a time
+// and none ahead.  32749 x 2304 bf16: first index 2 118 us, a pointer between 16-byte units 119, pitch 2305 158; f32, first index 1, 178.
 template <typename T, bool RES>
 __global__ void __launch_bounds__(256)
 dropout_any_kernel(const T *x, long long ldx, const T *res, long long ldr, T *y, long long ldy, long long rows, long long cols,

@@ -6,11 +6,13 @@
 // The scales change with every stage, so an accumulator cannot stay in TMEM over the whole reduction: each stage's partial
 // tile goes into the next of the TMEM buffers, the epilogue warps read it back while the following stages' products run,
 // and add it, scaled, to the tile they keep in registers (one fused multiply-add per entry and stage; one more product
-// where B's scales change from column to column).  What bounds it is this hand-over.  For a 256 x 256 tile of a CTA pair the
-// tensor cores alone take 750 cycles a stage (with the accumulator left in TMEM), TMEM read-back and additions 320 (580 with
-// column scales: two packed instructions per two entries, two cycles each); with two buffers a stage comes to 930 (1306):
-// a partial tile is complete 800 cycles after its products are issued, drained 400 (750) later, and its buffer's release
-// reaches the issuing thread another 200 later.  8192 x 8192 x 4096: 267 us, 2060 TFLOP/s; 317 under the power cap.
+// where B's scales change from column to column).  For a 256 x 256 tile of a CTA pair a stage takes 930 cycles (1306 with column
+// scales).  Measured one by one: the same loop without the hand-over 750 (the products are 510 of them, the delivery of the operands
+// probably the rest), TMEM read-back and additions alone 320 (580: two packed instructions per two entries, two cycles each).  A
+// partial tile is complete 800 cycles after its products are issued, drained 400 (750) later, and its buffer's release reaches the
+// issuing thread another 200 later; over two buffers that makes 700 (875) a stage, so 180 (430) are not accounted for by these parts.
+// 8192 x 8192 x 4096: 267 us, 2060 TFLOP/s; 315 to 320 under the power cap.  Between 5 and 128 rows a tile is mostly empty rows and
+// the time is latency: 4096 x 4096 8.9 us for 8 rows, 10.1 for 128 (5.6 for 4 rows in their own form).
 //
 // Tiles: 256 x 256 per CTA pair (cta_group::2, as in the index products), or 128 x 128 per CTA where that is estimated to be
 // faster (make_plan).  With few tiles (a short prompt) the reduced dimension is also cut over the CTAs of a cluster, whose

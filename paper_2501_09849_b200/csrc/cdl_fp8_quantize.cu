@@ -9,8 +9,8 @@
 // 128 consecutive columns, so loads and code stores are whole lines, and a row's maximum is four shuffles.  The transposed
 // codes go through 16 KB of shared memory in units of 8 rows, the unit number exclusive-ored with the column's, which
 // keeps both the stores (a thread has eight rows of one column) and the loads (a warp writes two columns) free of bank
-// conflicts.  HBM is the bound: 4 (bf16, both orientations) to 6 (f32) bytes per element: 8192 x 4096 bf16 both ways 25 us
-// (5.3 TB/s), 5001 x 4608 f32 blocks 26 us; 16-bit pieces unpacked into floats, at half the CTAs per SM, took 56 us.
+// conflicts.  HBM is the bound: 4 (bf16, both orientations) to 6 (f32) bytes per element: 8192 x 4096 bf16 both ways 26 us
+// (5.2 TB/s), 5001 x 4608 f32 blocks 26 us; 16-bit pieces unpacked into floats, at half the CTAs per SM, took 56 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -49,7 +49,7 @@ __device__ __forceinline__ uint32_t code2(float a, float b)
 }
 
 // Four words (eight 16-bit entries) from an address that is only aligned to its elements: the two 16-byte units they lie in,
-// shifted (3001 x 3003 bf16 both ways: 12.4 us, with loads of single entries 19.1; for f32 single entries are the faster
+// shifted (3001 x 3003 bf16 both ways: 10.6 to 12.4 us, with loads of single entries 19.1; for f32 single entries are the faster
 // form, 15.5 against 18.2).  The units may reach up to 14 bytes before and behind the words; the caller has seen that they
 // are inside the matrix.
 __device__ __forceinline__ void load_shifted(const void *p, uint32_t (&out)[4])

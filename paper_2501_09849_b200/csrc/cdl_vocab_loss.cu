@@ -9,8 +9,9 @@
 //   DW      dW = dl^T H     both MN-major      rows of this piece, final
 //   DH      dH += dl W      K-major, MN-major  summed over the pieces in a binary32 buffer, in their order
 // The backward pass recomputes the logits of a piece (2 T Vp D operations) rather than keep them: what is kept between the
-// two passes is lse, one float per row, and the piece's dl is small enough to stay in L2 between the product that
-// writes it and the two that read it.
+// two passes is lse, one float per row.  A piece's dl has 64 MB at most, and so stays in L2 between the product that writes it and
+// the two that read it, up to 16384 rows; a piece has 2048 words at least, so that with more rows dl grows, 4096 bytes a row, and goes
+// through HBM.
 //
 // The label's entry of dl is -g_t sum_{v != y_t} exp(l_tv - lse_t), never exp(l_ty - lse_t) - 1, where that would cancel: lse is a
 // binary32 number of the logits' size, so the difference from 1 is only good to 2^-24 |lse| (a loss of 1e-4 among logits of
@@ -24,8 +25,8 @@
 // in TMEM let the epilogue of a tile run beside the products of the next.  Where pairs would leave half of the device idle
 // (few rows, a small vocabulary) the statistics take 128-row tiles of one CTA, narrower ones if need be.  The backward pass
 // mixes the products that read one piece's dl with the product that writes the next one's in one launch, whose units are
-// spread over the pairs by their lengths: one ragged end per piece instead of three (4096 x 50176 x 2048: 2.85 -> 2.28 ms
-// together with a stage loop of its own for each kind of operands).
+// spread over the pairs by their lengths: one ragged end per piece instead of three (4096 x 50176 x 2048, forward and backward: 2.85 ->
+// 2.28 ms together with a stage loop of its own for each kind of operands; 2.6 to 2.7 under the power cap).
 // What bounds it: the tensor cores, 520 cycles a stage of 512 forward (92.5 % of their cycles, 1.66 PFLOP/s) and 608 backward
 // (86 %); below about 400 reduced entries the exponentials of the epilogue, 3300 cycles a tile (a special-function unit
 // takes eight per instruction and scheduler: 2112).  Rows that do not start on 128 bytes cost 725 cycles a stage.
@@ -763,7 +764,7 @@ struct LossPlan {
     size_t fwd_bytes, bwd_bytes;
 };
 constexpr size_t kOffScale = kStatusBytes, kOffData = kStatusBytes + 256;
-constexpr long long kPieceBytes = 64ll << 20;          // dl of one piece
+constexpr long long kPieceBytes = 64ll << 20;          // dl of one piece, where that is 2048 words or more
 constexpr long long kAccBytes = 64ll << 20;            // most that the splits of dH's product may add up to
 constexpr int kPlanSlots = 74;                         // B200: planned for this count so that workspace sizes are fixed
 
@@ -787,7 +788,7 @@ LossPlan make_plan(int T, int V, int D)
             }
         }
     }
-// With at most 128 rows a pair's second CTA would have nothing of dl or dH to do (16 x 3027 x 1958: 36 us of backward pass in pairs,
+    // With at most 128 rows a pair's second CTA would have nothing of dl or dH to do (16 x 3027 x 1958: 36 us of backward pass in pairs,
     // 28 in single CTAs; 64 x 5000 x 1500 40 and 32; 79 x 61013 x 182, all outputs and no reduction, 51 and 55).
     p.grad_pair = T > 128;
     const long long slots = p.grad_pair ? kPlanSlots : 2 * kPlanSlots, edge = p.grad_pair ? 256 : 128;
