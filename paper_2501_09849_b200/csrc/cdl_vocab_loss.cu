@@ -13,7 +13,7 @@
 // the two that read it, up to 16384 rows; a piece has 2048 words at least, so that with more rows dl grows, 4096 bytes a row, and goes
 // through HBM.
 //
-// The label's entry of dl is -g_t sum_{v != y_t} exp(l_tv - lse_t), never exp(l_ty - lse_t) - 1, where that would cancel: lse is a
+// The label's entry of dl is -g_t sum_{v != y_t} exp(l_tv - lse_t) where g_t (exp(l_ty - lse_t) - 1) would cancel: lse is a
 // binary32 number of the logits' size, so the difference from 1 is only good to 2^-24 |lse| (a loss of 1e-4 among logits of
 // 25: 0.5 % off, of 300: 10 %).  With one piece, DLOGIT adds up the other probabilities of its columns and loss_label_kernel puts
 // the entry into dl before it is read (2 to 4 us: 16 x 3027 x 1958 40.7 -> 42.9, 777 x 32003 x 1000 228 -> 231).  With several, dl of
@@ -443,11 +443,15 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                                 for (int c = 0; c < 32; ++c)
                                     if (c0 + 32 * h + c >= J) v[c] = 0u;           // a column that does not exist
                             }
-                            if (__any_sync(0xffffffffu, (unsigned)(label - (c0 + 32 * h)) < 32u)) {
+                            const bool here = __any_sync(0xffffffffu, (unsigned)(label - (c0 + 32 * h)) < 32u);
+                            float own = 0.0f;
+                            if (here) {
 #pragma unroll
                                 for (int c = 0; c < 32; ++c)
-                                    if (label == c0 + 32 * h + c)
-                                        v[c] = P.others != nullptr ? 0u : __float_as_uint(entry <= 0.0f ? entry * 16777216.0f : __uint_as_float(v[c]) - 16777216.0f);
+                                    if (label == c0 + 32 * h + c) {
+                                        own = __uint_as_float(v[c]);
+                                        v[c] = 0u;
+                                    }
                             }
                             if (P.others != nullptr) {
                                 float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
@@ -459,6 +463,12 @@ loss_gemm_kernel(const __grid_constant__ LossMaps maps, const __grid_constant__ 
                                     s3 += __uint_as_float(v[c + 3]);
                                 }
                                 others += (s0 + s1) + (s2 + s3);
+                            }
+                            if (here) {
+                                own = entry <= 0.0f ? entry * 16777216.0f : own - 16777216.0f;
+#pragma unroll
+                                for (int c = 0; c < 32; ++c)
+                                    if (label == c0 + 32 * h + c) v[c] = __float_as_uint(own);
                             }
 #pragma unroll
                             for (int c = 0; c < 16; ++c) {
@@ -619,7 +629,9 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
-// The labels' entries of dl, one piece: minus the sum of the other words' entries, a warp per row.
+// The labels' entries of dl, one piece, where the label has more than half of the probability: minus the sum of the other words' entries,
+// a warp per row.  (Where it has less, the difference from 1 that DLOGIT has written is the better one: probabilities are good to
+// lse's 2^-24 |lse|, which the sum has in proportion to the other words' share and the difference to the label's.)
 template <typename T>
 __global__ void __launch_bounds__(128)
 loss_label_kernel(const float *others, int parts, const long long *labels, const float *dloss, const float *scale, int rows, int V, T *dl, long long ld)
@@ -634,7 +646,7 @@ loss_label_kernel(const float *others, int parts, const long long *labels, const
     float s = 0.0f;
     for (int i = lane; i < parts; i += 32) s += others[row * parts + i];
     s = warp_sum(s);
-    if (lane == 0) dl[row * ld + y] = from_f32<T>(-s * g);
+    if (lane == 0 && s < 8388608.0f) dl[row * ld + y] = from_f32<T>(-s * g);     // (sums are in units of 2^-24)
 }
 
 // Several pieces: the rows whose label's probability is so close to 1 that its distance, taken from lse, is not good to 2^-10: where

@@ -106,3 +106,37 @@ def test_many_confident_rows_are_reproducible():
     ref = p @ w.double() / T
     # two independent roundings to 16 bits, row by row
     assert bool(((outs[0][2].double() - ref).norm(dim=1) <= 2 * 2.0 ** -8 * ref.norm(dim=1)).all())
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("T,V,D,seed", [(1, 4644, 1184, 1), (1, 700, 2000, 2), (2, 3000, 1504, 3), (3, 3000, 1504, 4), (200, 2000, 1600, 5)])
+def test_label_entries_of_improbable_words_are_minus_one(kind, T, V, D, seed):
+    """Logits in the hundreds, labels of next to no probability: the entry does not take part in the errors of the other probabilities."""
+    import torch
+    code, dtype, u = TYPES[kind]
+    dt = getattr(torch, dtype)
+    g = torch.Generator().manual_seed(seed)
+    h = (40 * torch.randn(T, D, generator=g)).to(dt)
+    w = (torch.randn(V, D, generator=g) * (1.5 / math.sqrt(D))).to(dt)
+    logits = h.double() @ w.double().t()
+    p = torch.softmax(logits, 1)
+    y = torch.empty(T, dtype=torch.int64)
+    taken = set()
+    for t in range(T):                       # an improbable word of its own, which no other row gives any probability
+        for v in torch.randperm(V, generator=g).tolist():
+            if float(p[:, v].max()) < 1e-12 and v not in taken:
+                y[t] = v
+                taken.add(v)
+                break
+    assert len(taken) == T
+    h, w, y = h.cuda(), w.cuda(), y.cuda()
+    gl = torch.full((T,), 1.0, device="cuda")
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    nb = cdl.cdl_vocab_loss_workspace_bytes(T, V, D, 1)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda")
+    cdl.cdl_vocab_loss_fwd(h, D, w, D, code, y, T, V, D, loss, lse, ws, nb)
+    cdl.cdl_vocab_loss_bwd(h, D, w, D, code, y, lse, gl, T, V, D, dh, D, dw, D, ws, nb)
+    cdl.cdl_workspace_status(ws)
+    # dl is -1, which has no rounding; the weights' gradient at the label is -h but for the other rows' 1e-12
+    assert bool(((dw[y].double() + h.double()).abs() <= h.double().abs() * u + 1e-9 * T).all())
