@@ -16,10 +16,10 @@
 // The label's entry of dl is -g_t sum_{v != y_t} exp(l_tv - lse_t) where g_t (exp(l_ty - lse_t) - 1) would cancel: lse is a
 // binary32 number of the logits' size, so the difference from 1 is only good to 2^-24 |lse| (a loss of 1e-4 among logits of
 // 25: 0.5 % off, of 300: 10 %).  With one piece, DLOGIT adds up the other probabilities of its columns and loss_label_kernel puts
-// the entry into dl before it is read (2 to 4 us: 16 x 3027 x 1958 40.7 -> 42.9, 777 x 32003 x 1000 228 -> 231).  With several, dl of
-// the first piece is consumed before the last is known: the rows whose label has a probability close to 1 (loss_confident_kernel)
-// are put together, and their other words' sums taken by STATS before the first piece (where there is no such row 9 us: 1024 x 100000
-// x 64 214 -> 225); the other rows' entries are good to 2^-10 as the difference.
+// the entry into dl before it is read (2 to 6 us: 16 x 3027 x 1958 40.7 -> 43.2, 777 x 32003 x 1000 222 -> 226, 79 x 61013 x 182 69 ->
+// 74).  With several, dl of the first piece is consumed before the last is known: the rows whose label has a probability close to
+// 1 (loss_confident_kernel) are put together, and their other words' sums taken by STATS before the first piece (where there is
+// no such row 9 to 17 us: 1024 x 100000 x 64 214 -> 227); the other rows' entries are good to 2^-10 as the difference.
 //
 // Tiles: 256 x 256 per CTA pair (cta_group::2), 64 reduced entries (128 bytes) per stage, six stages; two accumulators
 // in TMEM let the epilogue of a tile run beside the products of the next.  Where pairs would leave half of the device idle
