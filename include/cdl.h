@@ -536,8 +536,8 @@ int cdl_act_bwd(const void *dy, int64_t lddy, const void *codes, int64_t ldc, co
  *            `act` of: the gradient that leaves the layer before this one's activation.  act = CDL_ACT_NONE: no derivative, codes not read.
  *   weight   dW[n,k] = sum_m dY[m,n] A[m,k] (+ what dW holds, with accumulate),   dbias[n] = sum_m dY[m,n]
  * Products and sums in binary32, the epilogue in binary32, rounded once to out_type.  The tensor cores' sums are cut off, not rounded: over
- * 768 reduced entries at a time where out_type is CDL_F32, 1024 where z is kept (so that a 16-bit result can differ in its last place from
- * that of a call without codes), over all of them otherwise; from there on they are added rounded.
+ * 512 reduced entries at a time where out_type is CDL_F32, 1024 where it has 16 bits; from there on they are added rounded.  out does not
+ * depend on whether codes are asked for.
  *   A [dev] M x K, W [dev] N x K, dY [dev] M x N of `type` (CDL_BF16 or CDL_F16), 16-byte aligned, pitches multiples of 8.
  *   out, dA, dW [dev] and residual [dev] of out_type (any type), pitches in elements, aligned to their element; out, dA may be residual.
  *   bias, dbias [dev] N floats, nullable.  residual nullable.  codes [dev] 16-byte aligned, pitch ldc a multiple of 16 (M x N in the

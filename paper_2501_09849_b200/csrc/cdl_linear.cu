@@ -6,11 +6,12 @@
 // stored matrix is contiguous.
 //
 // The tensor cores' sums are cut off, not rounded, so an accumulator loses up to 2^-24 of itself with every instruction: over a
-// reduction of 8192 that is 1e-5.  So where a result is binary32 (a checkpoint's scales are) a tile is summed in segments, which the
-// epilogue warps take out of TMEM into registers (128 a thread) while the next segment's products run in the other half of TMEM: 12
-// stages, off by 7e-7 of the norm, 16 by 9e-7; a binary32 product by 3e-7 to 1e-6.  A segment's hand-over costs some 1200 cycles of the
-// products' 520 a stage, and the last one holds its half of TMEM during the epilogue (8192 x 8192 x 2048 with GELU and checkpoint 263 us,
-// in one segment 241 to 253, scales 2e-6 off); 16-bit results without a checkpoint are one segment.
+// reduction of 8192 that is 1e-5, and without a limit where the reduction has none.  So a tile is summed in segments, which the
+// epilogue warps take out of TMEM into registers (128 a thread) while the next segment's products run in the other half of TMEM: 8
+// stages where the result is binary32, off by 4.8e-7 of the norm (12 by 7e-7; a binary32 product by 3e-7 to 1e-6), 16 where it has 16
+// bits, by 9e-7, with a checkpoint or without, so that the result is the same.  A segment's hand-over costs some 1200 cycles of the
+// products' 520 a stage, and the last one holds its half of TMEM during the epilogue: 8192 x 8192 x 2048 to 16 bits 212 us, with GELU and
+// checkpoint 262, to binary32 254; 16-bit results in one segment 205 and 241 to 253, binary32 ones in segments of 12 stages 243.
 // A finished tile leaves TMEM a row a lane, 32 columns at a time, and goes out by TMA; where the output's rows do not start on 16 bytes it is
 // turned through shared memory and stored with neighbouring lanes on neighbouring columns.
 // Tiles: 256 x 256 per CTA pair (cta_group::2), or 128 x 128 per CTA where there are few; 64 reduced entries (128 bytes) a stage.
@@ -43,8 +44,8 @@ constexpr int kThreads = 128 + 32 * kEpiWarps;         // a warpgroup that feeds
 constexpr int kRegsLaunch = 168, kRegsDrive = 88, kRegsEpilogue = 208;
 static_assert(128 * kRegsDrive + 32 * kEpiWarps * kRegsEpilogue <= kThreads * kRegsLaunch, "register shares");
 constexpr int kBK = 64;                                // reduced entries of a stage (128 bytes)
-// Stages that are summed in TMEM: for binary32 results, and for 16-bit results with a checkpoint.
-constexpr int kSegment = 12, kKeepSegment = 16;
+// Stages that are summed in TMEM, for binary32 and for 16-bit results.
+constexpr int kSegment32 = 8, kSegment16 = 16;
 constexpr int kSlope = 8;                              // + CDL_ACT_*: the derivative instead of the activation
 constexpr int kBlockBytes = 128 * 128;                 // operand block of 128 rows
 constexpr int kOutWarpBytes = 32 * 128;
@@ -378,7 +379,7 @@ __device__ __forceinline__ void finish_row(const LinearOut &E, long long row, in
     linear_store<4>(E, row, col, step, in, v);
 }
 
-// RUNS: some tiles are cut into runs of stages.  SEGMENT: stages after which sums are taken out of TMEM, or 0.
+// RUNS: some tiles are cut into runs of stages.  SEGMENT: stages after which sums are taken out of TMEM.
 // SPLIT: a tile is a cluster's, whose CTAs share its stages; their sums go to shared memory, and each CTA finishes a part of the rows over
 // all of them, in the order of the CTAs.
 template <bool PAIR, bool RUNS, int SEGMENT, bool SPLIT>
@@ -511,7 +512,6 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
                 constexpr bool kA = decltype(a_mn)::value, kB = decltype(b_mn)::value;
                 const uint32_t a_lo0 = kA ? mn_lo : k_lo, b_lo0 = (kB ? mn_lo : k_lo) + (uint32_t)(kBlockBytes >> 4);
                 const uint32_t idesc = idesc0 | ((kA ? 1u : 0u) << 15) | ((kB ? 1u : 0u) << 16);
-                const int most = SEGMENT > 0 ? SEGMENT : count;
                 while (count > 0) {
                     const uint32_t te = tempty0 + 8u * buf;
                     if (!mbar_try_wait_now(te, tpar) && !mbar_wait(te, tpar, abort_flag, kWaitNs)) {
@@ -519,7 +519,7 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
                         return;
                     }
                     uint32_t accumulate = 0u;
-                    for (int i = SEGMENT > 0 ? min(count, most) : most; i > 0; --i) {
+                    for (int i = min(count, SEGMENT); i > 0; --i) {
                         const uint32_t fb = bar0 + 8u * st;
                         if (!mbar_try_wait_now(fb, par) && !mbar_wait(fb, par, abort_flag, kWaitNs)) {
                             failed = true;
@@ -540,7 +540,7 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
                     else tc_commit(tfull0 + 8u * buf);
                     buf ^= 1u;
                     if (buf == 0u) tpar ^= 1u;
-                    count -= most;
+                    count -= SEGMENT;
                 }
             };
             for (int u = first_tile; u < tail_end && !failed; u = next_tile(u)) {
@@ -586,7 +586,7 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
             };
             bool added = false;                            // the bias is in the sums, and `peak` is their rows' largest magnitude
             float peak = 0.0f;
-            if (SEGMENT > 0 && kb1 - kb0 > SEGMENT) {
+            if (kb1 - kb0 > SEGMENT) {
                 // the segments' sums, in registers; then back to where the last one's were, so that the epilogue is one
                 float acc[kHalf];
 #pragma unroll
@@ -983,9 +983,9 @@ int launch_linear(int mode, const void *A, int64_t lda, const void *B, int64_t l
     {reinterpret_cast<const void *>(&linear_kernel<false, false, SEGMENT, false>), reinterpret_cast<const void *>(&linear_kernel<true, false, SEGMENT, false>), \
      reinterpret_cast<const void *>(&linear_kernel<false, true, SEGMENT, false>), reinterpret_cast<const void *>(&linear_kernel<true, true, SEGMENT, false>),   \
      reinterpret_cast<const void *>(&linear_kernel<false, false, SEGMENT, true>)}
-    static const void *const kernels[3][5] = {CDL_FORMS(0), CDL_FORMS(kSegment), CDL_FORMS(kKeepSegment)};
+    static const void *const kernels[2][5] = {CDL_FORMS(kSegment32), CDL_FORMS(kSegment16)};
 #undef CDL_FORMS
-    const void *const kernel = kernels[E.type == CDL_F32 ? 1 : (E.codes != nullptr ? 2 : 0)][plan.splits > 1 ? 4 : (plan.pair ? 1 : 0) + (plan.ranges > 0 ? 2 : 0)];
+    const void *const kernel = kernels[E.type == CDL_F32 ? 0 : 1][plan.splits > 1 ? 4 : (plan.pair ? 1 : 0) + (plan.ranges > 0 ? 2 : 0)];
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -997,13 +997,13 @@ int launch_linear(int mode, const void *A, int64_t lda, const void *B, int64_t l
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmemBytes;
     if (!attr_set[dev]) {
-        for (int v = 0; v < 15; ++v)
+        for (int v = 0; v < 10; ++v)
             if (cudaFuncSetAttribute(kernels[v / 5][v % 5], cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) {
                 (void)cudaGetLastError();
                 return CDL_ERR_LAUNCH;
             }
         // the warpgroups' shares must fit what a block is launched with, or an epilogue warpgroup would wait for good
-        for (int v = 0; v < 15; ++v) {
+        for (int v = 0; v < 10; ++v) {
             cudaFuncAttributes fa;
             if (cudaFuncGetAttributes(&fa, kernels[v / 5][v % 5]) != cudaSuccess || fa.numRegs < kRegsLaunch) {
                 (void)cudaGetLastError();
