@@ -2,7 +2,8 @@
 //
 // Bound by reading W once.  A warp takes sixteen rows of W and multiplies 32 reduced entries by two m16n8k16 matrix instructions whose
 // first operand is W and whose eight columns are the rows of A: a lane's part of either is eight consecutive entries of a row (any order
-// of the reduced entries will do as long as both operands have the same).  Sums are binary32.
+// of the reduced entries will do as long as both operands have the same).  The instructions' binary32 sums are cut off, not rounded, so they
+// are added up after 512 entries (in one go 8 x 4655 x 60000 was off by 8e-6 of the norm).
 // W comes through shared memory by 16-byte asynchronous copies, kSlots - 1 steps of 128 entries ahead; a lane fetches what it reads
 // itself: no barrier, and any length.  The warps of a CTA share the reduced dimension when there are few rows of W, and are added in
 // their order.
@@ -22,6 +23,7 @@ constexpr int kRowsPerWarp = 16;
 constexpr int kWarps = 16;              // most warps of a CTA
 constexpr int kStep = 128;              // entries of the reduced dimension that a warp fetches together
 constexpr int kPieces = kStep / 32;     // ... in pieces of 32: four lanes of eight entries
+constexpr int kSegment = 4;             // steps that the matrix instructions sum
 constexpr int kSlots = 3;               // steps on their way or in use
 constexpr int kSlotBytes = kRowsPerWarp * kStep * 2;
 constexpr int kWarpSmem = kSlots * kSlotBytes;
@@ -113,7 +115,7 @@ linear_rows_kernel(RowsParams P)
     for (int s = 0; s < kSlots - 1; ++s) ask();
     int slot = 0;
     for (int pass = 0; pass < P.passes; ++pass) {
-        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float c[4] = {0.0f, 0.0f, 0.0f, 0.0f}, part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         // what the epilogue reads is on its way before the first entries of W are
         LinearIn<1> in[4];
         float bias[4];
@@ -145,9 +147,15 @@ linear_rows_kernel(RowsParams P)
             for (int i = 0; i < kPieces; ++i) {
                 const uint4 q0 = lds_u128(at + (uint32_t)(i * 512)), q1 = lds_u128(at + (uint32_t)((kPieces + i) * 512));
                 if (!has_row) x[i] = make_uint4(0u, 0u, 0u, 0u);
-                mma_16<T>(c, q0.x, q1.x, q0.y, q1.y, x[i].x, x[i].y);
-                mma_16<T>(c, q0.z, q1.z, q0.w, q1.w, x[i].z, x[i].w);
+                mma_16<T>(part, q0.x, q1.x, q0.y, q1.y, x[i].x, x[i].y);
+                mma_16<T>(part, q0.z, q1.z, q0.w, q1.w, x[i].z, x[i].w);
             }
+            if (j % kSegment == kSegment - 1 || j == count - 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    c[i] += part[i];
+                    part[i] = 0.0f;
+                }
         }
         if (P.slices > 1) {
 #pragma unroll

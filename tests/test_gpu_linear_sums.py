@@ -93,3 +93,17 @@ def test_weight_gradients_over_many_rows(M, N, K, form):
             # for entries below the norm's
             assert float((dw != ref.half()).double().mean()) <= 0.01
 
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K", [(8, 1000, 3000), (3, 4655, 40000), (8, 4655, 60000), (5, 30000, 2280)])
+def test_few_rows(kind, M, N, K):
+    """The same bound where one to eight rows have a form of their own, whose warps take up to 7500 reduced entries each here."""
+    import torch
+    assert forward_form(M, N, K) == "rows"
+    f = Forward(torch, kind, M, N, K)
+    ref = f.exact()
+    assert float((f.run("f32", bias=False).double() - ref).norm() / ref.norm()) <= 7e-7
+    gb = -(-N // 128)
+    largest = torch.nn.functional.pad(ref.abs(), (0, gb * 128 - N)).view(M, gb, 128).amax(2).t() / 448
+    scales = f.run(kind, bias=False, keep=True)[2].double()
+    assert float((scales - largest).norm() / largest.norm()) <= 1.4e-6
