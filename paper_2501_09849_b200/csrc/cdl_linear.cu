@@ -255,9 +255,10 @@ __device__ __forceinline__ RowsIn<HALF> ask_rows(const LinearOut &E, int lane, i
 }
 
 // 32 rows x HALF columns of finished sums in TMEM at `taddr`.  Where two warps share a checkpoint's groups of 128, they exchange their rows'
-// largest magnitudes through `peaks` ([half][row of the tile]).  added: the bias is in the sums already, and `peak` is known.
+// largest magnitudes through `peaks` ([half][row of the tile]); false where the other one does not come.  added: the bias is in the sums already,
+// and `peak` is known.
 template <int HALF>
-__device__ __forceinline__ void emit_rows(const LinearParams &P, const CUtensorMap *map_o, const RowsIn<HALF> &in, bool added, float peak, float *peaks, int quarter, uint32_t taddr, uint32_t wbuf, uint32_t &turn, int lane, int row0, int col0)
+__device__ __forceinline__ bool emit_rows(const LinearParams &P, const CUtensorMap *map_o, const RowsIn<HALF> &in, bool added, float peak, float *peaks, PeakExchange &exchange, volatile int *abort_flag, int quarter, uint32_t taddr, uint32_t wbuf, uint32_t &turn, int lane, int row0, int col0)
 {
     const LinearOut &E = P.out;
     const int row = row0 + lane;
@@ -284,10 +285,7 @@ __device__ __forceinline__ void emit_rows(const LinearParams &P, const CUtensorM
         const int half = HALF == 64 ? (col0 >> 6) & 1 : 0;
         if (HALF == 64 && (half == 1 || col0 + HALF < E.J)) {      // (the other warp is there)
             float *at = peaks + quarter * 32 + lane;
-            asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");      // (the last tile's have been read)
-            at[half * 128] = m;
-            asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
-            m = fmaxf(m, at[(half ^ 1) * 128]);
+            if (!exchange(at + half * 128, at + (half ^ 1) * 128, lane, m, abort_flag, kWaitNs)) return false;
         }
         fp8_scale_of(m, s, rrec);
         if (live && half == 0) E.scales[(long long)(col0 >> 7) * E.I + row] = s;
@@ -354,6 +352,7 @@ __device__ __forceinline__ void emit_rows(const LinearParams &P, const CUtensorM
         else if (E.type == CDL_BF16) copy_piece<__nv_bfloat16>(E, v, wbuf, lane, row0, c0);
         else copy_piece<__half>(E, v, wbuf, lane, row0, c0);
     }
+    return true;
 }
 
 // 128 columns of a row by a warp, four columns a lane (or every 32nd, where rows do not start on four entries): sums, the bias and the
@@ -394,6 +393,7 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
     __shared__ uint32_t tmem_base_s, asked_s;
     __shared__ int abort_s;
     __shared__ float peaks[PAIR ? 1 : 2 * 128];
+    __shared__ __align__(8) unsigned char meet[PAIR ? 8 : 4 * PeakExchange::kBytes];
 
     const uint32_t smem_base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -437,6 +437,8 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
             mbar_init(tfull0 + 8u * b, 1);
             mbar_init(tempty0 + 8u * b, PAIR ? 2 * kEpiWarps : kEpiWarps);
         }
+        if (!PAIR)
+            for (int q = 0; q < 4; ++q) PeakExchange::init(smem_u32(meet) + (uint32_t)q * PeakExchange::kBytes);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc_all<PAIR>(smem_u32(&tmem_base_s));
@@ -562,6 +564,7 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
         const uint32_t wbuf = smem_base + (uint32_t)kRingBytes + (uint32_t)((warp - 4) * kOutWarpBytes);
         const LinearOut &E = P.out;
         uint32_t buf = 0u, tpar = 0u, turn = 0u;
+        PeakExchange exchange{smem_u32(meet) + (PAIR ? 0u : (uint32_t)quarter * PeakExchange::kBytes), 0u};
         for (int u = first_tile; u < tail_end && !failed; u = next_tile(u)) {
             int ti, tj, kb0, kb1;
             tile_at(u, P.tiles_i, P.tiles_j, ti, tj);
@@ -662,8 +665,12 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
                             for (int q = 0; q < 8; ++q)
                                 put_unit(smem_base + (uint32_t)r * 512u + (uint32_t)((((in_col + c) / 4 + q) ^ (r & 7)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
                     }
-                } else if (!RUNS || kb1 - kb0 == P.KB) emit_rows<kHalf>(P, &maps.o, in, added, peak, peaks, quarter, taddr, wbuf, turn, lane, row0, col0);
-                else {
+                } else if (!RUNS || kb1 - kb0 == P.KB) {
+                    if (!emit_rows<kHalf>(P, &maps.o, in, added, peak, peaks, exchange, abort_flag, quarter, taddr, wbuf, turn, lane, row0, col0)) {
+                        failed = true;
+                        break;
+                    }
+                } else {
                     // a part of a tile: its sums as they are, through the staging buffer 32 columns at a time
 #pragma unroll 1
                     for (int ch = 0; ch < kHalf / 32 && col0 + ch * 32 < E.J; ++ch) {
@@ -752,9 +759,6 @@ linear_kernel(const __grid_constant__ LinearMaps maps, const __grid_constant__ L
     if (failed) {
         abort_s = 1;
         if (lane == 0) record_timeout(P.status);
-        // (a warp that has given up meets the other one of its rows, which may wait for its peaks)
-        if (!PAIR && warp >= 4 && P.out.codes != nullptr)
-            for (int i = 0; i < 2; ++i) asm volatile("bar.arrive %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
     }
     tc_fence_before();
     __syncthreads();

@@ -81,6 +81,33 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// Two warps exchange a number a lane, each time they meet: the larger one of both to both.  Bounded like every wait: a warp whose partner does
+// not come, or has set the abort flag, gets false.  (A named barrier has no limit, and two arrivals of one warp complete it.)
+struct PeakExchange {
+    static constexpr uint32_t kBytes = 16;      // two mbarriers of two arrivals each: the numbers are there, the numbers have been read
+    uint32_t bars, turn;
+    static __device__ __forceinline__ void init(uint32_t bars)
+    {
+        mbar_init(bars, 2);
+        mbar_init(bars + 8u, 2);
+    }
+    // mine, other: this lane's place and the other warp's.  All lanes call.
+    __device__ __forceinline__ bool operator()(float *mine, const volatile float *other, int lane, float &m, volatile int *abort_flag, unsigned long long limit_ns)
+    {
+        auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_try_wait_now(bar, parity) || mbar_wait(bar, parity, abort_flag, limit_ns)) != 0; };
+        if (!wait(bars + 8u, turn ^ 1u)) return false;      // (before the first time: at once)
+        *mine = m;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars);
+        if (!wait(bars, turn)) return false;
+        m = fmaxf(m, *other);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars + 8u);
+        turn ^= 1u;
+        return true;
+    }
+};
+
 // The loads of the last `stages` of `asked` ring stages, whose barriers are at bar + 8 * (stage % stages): waits until they have
 // landed, for at most 10 ms each (a load on its own takes microseconds; one that another CTA never issued does not come).
 __device__ __forceinline__ void drain_stages(uint32_t bar, uint32_t asked, uint32_t stages)
