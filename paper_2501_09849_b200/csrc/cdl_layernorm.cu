@@ -277,6 +277,9 @@ struct Feed {
     }
 };
 
+// 1 / sqrt(v + eps) from the mean of the deviations and that of their squares; a NaN stays one.
+__device__ __forceinline__ float rstd_of(float left, float square, float eps) { return 1.0f / sqrtf(max_nan(fmaf(-left, left, square), 0.0f) + eps); }
+
 // SHARED: a row is shared by the blocks of a cluster.
 template <typename T, bool VEC, int UNITS, int G, bool SHARED>
 __global__ void __launch_bounds__(fwd_threads(G), fwd_blocks(G, UNITS))
@@ -364,7 +367,7 @@ norm_fwd_kernel(const NormDev P)
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             const float left = d2[2 * k] * P.inv;           // what the mean's rounding left
-            r[k] = 1.0f / sqrtf(fmaxf(fmaf(-left, left, d2[2 * k + 1] * P.inv), 0.0f) + P.eps);
+            r[k] = rstd_of(left, d2[2 * k + 1] * P.inv, P.eps);
             d2[2 * k] = left;
             if (t == 0 && rank == 0 && row + k * step < P.rows) {
                 if (P.mean != nullptr) P.mean[row + k * step] = s[k] + left;
@@ -468,7 +471,7 @@ norm_fwd_long_kernel(const NormDev P)
         }
         sum2(d2);
         const float left = d2[0] * P.inv;
-        const float r = 1.0f / sqrtf(fmaxf(fmaf(-left, left, d2[1] * P.inv), 0.0f) + P.eps);
+        const float r = rstd_of(left, d2[1] * P.inv, P.eps);
         if (threadIdx.x == 0) {
             if (P.mean != nullptr) P.mean[row] = m0 + left;
             if (P.rstd != nullptr) P.rstd[row] = r;

@@ -28,3 +28,20 @@ def test_gradient_of_a_row_whose_mean_times_rstd_overflows(kind, cols):
     # a thread adds at most cols / 512 + 32 terms one after the other, then ten exchanges
     assert bool(((dx.double() - ref).abs() <= ref.abs() * u + size * (cols / 512 + 64) * 2.0 ** -24).all())
     assert bool((dg == 0).all()) and bool(((db.double() - dy.double().sum(0)).abs() <= dy.double().abs().sum(0) * 8 * 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("cols", COLS[1:] + [140001])
+def test_statistics_of_a_row_that_is_not_finite(kind, cols):
+    """mean and rstd of a row with a NaN or an infinity are NaN, or an infinity the mean, as the row is NaN; the other rows keep theirs."""
+    import torch
+    code, dtype, _ = TYPES[kind]
+    x = torch.randn(6, cols, generator=torch.Generator().manual_seed(2)).to(getattr(torch, dtype)).cuda()
+    y, clean = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd, m0, r0 = (torch.empty(6, device="cuda") for _ in range(4))
+    cdl.cdl_layernorm_fwd(x, cols, code, None, None, 6, cols, 1e-5, clean, cols, m0, r0)
+    x[1, cols // 2], x[3, cols - 1], x[4, 0] = float("nan"), float("inf"), float("-inf")
+    cdl.cdl_layernorm_fwd(x, cols, code, None, None, 6, cols, 1e-5, y, cols, mean, rstd)
+    bad, good = [1, 3, 4], [0, 2, 5]
+    assert bool(y[bad].isnan().all()) and bool(rstd[bad].isnan().all()) and not bool(mean[bad].isfinite().any())
+    assert torch.equal(y[good], clean[good]) and torch.equal(mean[good], m0[good]) and torch.equal(rstd[good], r0[good])
