@@ -483,7 +483,7 @@ size_t cdl_vocab_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t w
 /*
  * Layer norm of the rows of x:
  *   m = mean_c x[r,c],  v = mean_c (x[r,c] - m)^2,  s = 1 / sqrt(v + eps),  y[r,c] = (x[r,c] - m) * s * gamma[c] + beta[c]
- * Computed in binary32 and rounded once.  A row with a NaN or an infinity is NaN.
+ * Computed in binary32 and rounded once.  A row with a NaN or an infinity is NaN, and so is its rstd.
  *   x, y [dev] rows x cols of `type`, pitches ldx, ldy (not read when rows = 1), aligned to their element (16-byte alignment of bases and
  *   pitches takes the vector path); y may be x.  gamma, beta [dev] cols floats, each nullable (1 and 0).
  *   mean, rstd [dev] rows floats, each nullable: m and s, which the backward call takes.
@@ -492,7 +492,8 @@ size_t cdl_vocab_loss_workspace_bytes(int32_t T, int32_t V, int32_t D, int32_t w
  *   dx = rstd * (a - mean_c a - n * mean_c(a n)) (+ residual),   dgamma[c] = sum_r dy n,   dbeta[c] = sum_r dy
  *   dy, x, residual, dx [dev] rows x cols of `type`; residual nullable (the gradient that reaches x around the norm); dx may be dy or
  *   residual.  dx, dgamma, dbeta each nullable, one at least.  dgamma, dbeta [dev] cols floats, overwritten; rows = 0 clears them.
- *   ws [dev]: cdl_layernorm_workspace_bytes(rows, cols) bytes, 256-byte aligned; only with dgamma or dbeta.
+ *   ws [dev]: cdl_layernorm_workspace_bytes(rows, cols) bytes, 256-byte aligned; only with dgamma or dbeta.  Calls
+ *   that can overlap on the GPU need a workspace each.
  * The sums over the rows have a fixed order.
  */
 int cdl_layernorm_fwd(const void *x, int64_t ldx, int32_t type, const float *gamma, const float *beta, int32_t rows, int32_t cols,
@@ -503,7 +504,9 @@ int cdl_layernorm_bwd(const void *dy, int64_t lddy, const void *x, int64_t ldx, 
 size_t cdl_layernorm_workspace_bytes(int32_t rows, int32_t cols);
 
 /*
- * Activations.  NaN gives NaN; at -infinity the last three give their limit 0.
+ * Activations.  NaN gives NaN; at -infinity the last three give their limit 0.  Off by less than 5e-7 of the value in binary32 down to z = -1, below that
+ * by what rounding the exponential's argument costs: 9e-7, 2e-6 and 8e-6 at -4, -6 and -12 (CDL_ACT_GELU), 1.1e-6, 4e-6 and 1.2e-5 at -4, -6 and -10
+ * (CDL_ACT_GELU_TANH), 1e-6 and 4e-6 at -12 and -80 (CDL_ACT_SILU).
  */
 #define CDL_ACT_NONE 0
 #define CDL_ACT_RELU 1      /* max(z, 0); derivative 0 at 0 */

@@ -8,8 +8,11 @@
 // NaN gives NaN; at -infinity the values are their limit 0.
 //
 // F(z) for z < 0 is exp(-z^2 / 2) t P(t), t = 1 / (1 + 0.35 |z|), P a polynomial of degree 8 fitted here to 0.5 erfcx(|z| / sqrt 2) / t for
-// the least relative error over 0 <= |z| <= 14.5 (3.2e-8; evaluated in binary32 3.3e-7 of F).  The tail keeps its relative accuracy, where
-// 0.5 (1 + erf) would cancel.  Two special-function operations per entry in every activation.
+// the least relative error over 0 <= |z| <= 14.5 (3.2e-8).  There is no cancellation in the tail, where 0.5 (1 + erf) would have it; what the tail
+// loses is the exponential's argument, which is rounded to binary32 twice, some z^2 2^-24 of the value.  Largest relative errors of the values in
+// binary32, two million numbers a range: gelu 4.3e-7 for |z| up to 1, at z down to -2 5.0e-7, -4 8.6e-7, -6 2.0e-6, -8 3.1e-6, -12 7.6e-6, below 1e-7
+// from 1 on; gelu_tanh 2.8e-7, 4.7e-7, 1.1e-6, 3.9e-6, 8.2e-6, and 1.2e-5 at -10; silu 2.2e-7 up to 1, 3.4e-7 at -4, 9.3e-7 at -12, 3.8e-6 at -80.
+// Two special-function operations per entry in every activation.
 #pragma once
 #include <cuda_fp16.h>
 #include <float.h>

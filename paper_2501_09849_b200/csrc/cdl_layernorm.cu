@@ -12,8 +12,9 @@
 // The next rows are on their way to shared memory in 16-byte asynchronous copies, three of them (one in binary32): with one row ahead in
 // registers 8192 x 4096 took 87 us backward (spilled) and 33 forward.  A thread fetches what it reads itself; where rows do not start
 // on 16 bytes the row's units are copied as they lie, and the threads take every G-th entry of it behind a barrier.
-// 8192 x 4096 bf16: forward 28 us (4.8 TB/s), backward 42 (4.8), with a residual 50 (5.4); 4095 columns 47 and 63.  5000 x 4096 binary32:
-// 28 (5.8) and with a residual 54 (6.1).  Rows of 8193 columns are shared by two blocks that use half their threads: 2500 of them 44 and 110 us, of 8192 21 and 34.
+// 8192 x 4096 bf16: forward 29 us (4.6 TB/s), backward 43 (4.7), with a residual 50 (5.4); 4095 columns 44 and 62.  5000 x 4096 binary32:
+// 28 (5.8) and with a residual 54 (6.1).  Beyond 8192 columns a block takes four units a thread forward, half of which a row of 8200 does not have, and two
+// blocks share a row backward, with half of their threads: 2500 rows of 8192 columns 21 and 31 us, of 8200 33 and 77, of 8193 (unaligned) 44 and 101.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <float.h>
