@@ -14,6 +14,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "cdl_act.cuh"
 #include "cdl_internal.h"
 #include "cdl_lowp.cuh"
 
@@ -21,8 +22,6 @@ namespace cdl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kInvMax = 1.0f / 448.0f;
-constexpr float kTiny = 1.17549435e-38f;      // 2^-126
 
 struct QuantFp8 {
     const void *x;
@@ -33,20 +32,6 @@ struct QuantFp8 {
     long long ldc, ldt;
     float *scales, *scales_t;
 };
-
-__device__ __forceinline__ void scale_of(float amax, float &s, float &r)
-{
-    s = fmaxf(__fmul_rn(amax, kInvMax), kTiny);
-    r = __frcp_rn(s);
-}
-
-// codes of two values, the first in the low byte (saturating; NaN becomes the NaN code)
-__device__ __forceinline__ uint32_t code2(float a, float b)
-{
-    uint16_t w;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(w) : "f"(b), "f"(a));
-    return w;
-}
 
 // A thread's 8 x 8 piece of the tile: 64 floats, or 32 words of two 16-bit values, whose magnitudes are compared two at a
 // time.  Maxima drop a NaN: it does not enter a group's scale.
@@ -193,7 +178,7 @@ quantize_fp8_kernel(const QuantFp8 Q)
 #pragma unroll
         for (int k = 0; k < 8; ++k) m = fmaxf(m, part[k][0]);
         float s, r;
-        scale_of(m, s, r);
+        fp8_scale_of(m, s, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) rrec[i] = crec[i] = r;
         if (threadIdx.x == 0) {
@@ -221,7 +206,7 @@ quantize_fp8_kernel(const QuantFp8 Q)
         m[0] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, send, 2));
         m[0] = fmaxf(m[0], __shfl_xor_sync(0xffffffffu, m[0], 1));
         float s, r;
-        scale_of(fmaxf(m[0], 0.0f), s, r);
+        fp8_scale_of(fmaxf(m[0], 0.0f), s, r);
         const int mine = tx >> 1;                                // the row this lane was left with
         if ((tx & 1) == 0 && row + mine < Q.rows) Q.scales[(long long)tj * Q.rows + row + mine] = s;
 #pragma unroll
@@ -232,7 +217,7 @@ quantize_fp8_kernel(const QuantFp8 Q)
                 float mc = part[0][threadIdx.x];
 #pragma unroll
                 for (int k = 1; k < 8; ++k) mc = fmaxf(mc, part[k][threadIdx.x]);
-                scale_of(mc, s, r);
+                fp8_scale_of(mc, s, r);
                 part[0][threadIdx.x] = r;
                 if (c0 + (int)threadIdx.x < Q.cols) Q.scales_t[(long long)ti * Q.cols + c0 + threadIdx.x] = s;
             }
@@ -244,7 +229,7 @@ quantize_fp8_kernel(const QuantFp8 Q)
             if (row + i >= Q.rows) break;
             uint32_t h[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = code2(__fmul_rn(v.value(i, 2 * j), rrec[i]), __fmul_rn(v.value(i, 2 * j + 1), rrec[i]));
+            for (int j = 0; j < 4; ++j) h[j] = fp8_code2(__fmul_rn(v.value(i, 2 * j), rrec[i]), __fmul_rn(v.value(i, 2 * j + 1), rrec[i]));
             unsigned char *p = Q.codes + (long long)(row + i) * Q.ldc + col;
             if (col + 8 <= Q.cols) *reinterpret_cast<uint2 *>(p) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
             else
@@ -264,7 +249,7 @@ quantize_fp8_kernel(const QuantFp8 Q)
         for (int j = 0; j < 8; ++j) {
             uint32_t h[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = code2(__fmul_rn(v.value(2 * i, j), crec[j]), __fmul_rn(v.value(2 * i + 1, j), crec[j]));
+            for (int i = 0; i < 4; ++i) h[i] = fp8_code2(__fmul_rn(v.value(2 * i, j), crec[j]), __fmul_rn(v.value(2 * i + 1, j), crec[j]));
             *reinterpret_cast<uint2 *>(&tile_t[(tx * 8 + j) * 128 + ((ty ^ tx) << 3)]) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
         }
         __syncthreads();
