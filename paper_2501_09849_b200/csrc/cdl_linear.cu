@@ -17,7 +17,7 @@
 // Tiles: 256 x 256 per CTA pair (cta_group::2), or 128 x 128 per CTA where there are few; 64 reduced entries (128 bytes) a stage.
 // The stages of a last, partly filled round are one sequence, cut into as many runs as there are CTAs (pairs); tiles that runs share
 // are added in the order of the runs, and finished, by a second kernel.  One to eight rows of A have a form of their own.
-// Bound by the tensor cores, and under load by the power cap (8192 x 8192 x 2048 209 us, 1320 TFLOP/s; 8192^3 853 us); with much epilogue
+// Bound by the tensor cores, and under load by the power cap (8192 x 8192 x 2048 212 us, 1300 TFLOP/s; 8192^3 797 to 814 us); with much epilogue
 // and few reduced entries by its instructions (64 reduced entries: 42 us, with GELU 82).  Every wait is bounded.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
